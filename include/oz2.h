@@ -308,6 +308,81 @@ oz2_status oz2_ctx_last_gemm_launches(oz2_context *ctx, int64_t *launches);
 oz2_status oz2_ctx_release(oz2_context *ctx);    /* frees what the context owns on the device, keeps the context */
 
 /*
+ * Products in 8-bit floating point, for the layers of neural networks that are trained or served in it.  They share
+ * the conventions above (row-major, device pointers, asynchronous on `stream`, contexts) and nothing
+ * of Algorithm 1: an entry is one E4M3 number, a block of 128 has one power of two.
+ *
+ * oz2_f8: a rows x k matrix of E4M3 bytes (sign, 4 bits of exponent, 3 of fraction, largest 448, no infinities, NaN 0x7f and
+ * 0xff), entry (r, h) standing for q[r * ld + h] * 2^(s - 127), s = scale[(r / block_rows) * ld_scale + h / 128]; s = 255 stands
+ * for NaN.  block_rows is 1 or 128.  q is 16-byte aligned and ld a multiple of 16, at least k and at most 2^23; scale is
+ * 4-byte aligned and ld_scale a multiple of 4, at least ceil(k / 128).  Rows are stored up to the next multiple of 16
+ * bytes (of 4 scales): what lies between is read and has no effect.  The struct is read during the call only.
+ *
+ * Sums are held in binary32 by the matrix cores, which cut the products of 8 consecutive k (from a multiple of 8 on) towards zero at
+ * 2^-13 of the largest of the 8: a sum is off by less than 2^-10 sum |a||b|, for normal data by about 1.4e-5 of the norm of C.
+ * The E4M3 numbers themselves are rounded at 2^-4.  Results are rounded to their type once.  The order of the sums depends on the sizes and on whether the
+ * workspace has room for the planes of K ranges (oz2_f8_workspace_bytes), on nothing else: a call repeated gives the same bits.
+ * NaN in an entry reaches the entries of C that it belongs to.  m == 0 or n == 0: nothing is done.  k up to 2^20.
+ */
+typedef struct {
+    void *q;
+    int64_t ld;
+    void *scale;
+    int64_t ld_scale;
+    int block_rows;
+} oz2_f8;
+typedef enum { OZ2_BF16 = 0, OZ2_F16 = 1, OZ2_F32 = 2 } oz2_type;
+typedef enum { OZ2_ACT_SILU = 0, OZ2_ACT_GELU = 1 } oz2_act;   /* g / (1 + exp(-g)); the tanh form of GELU */
+
+/*
+ * X (rows x cols numbers of `type`, ldx >= cols) in 8 bits: as it is, transposed (cols x rows), or both from one read; the other
+ * pointer is NULL.  Both have the same block_rows; blocks of one row run along the rows of what is written, so those of
+ * the transpose run down the columns of X.  The scale of a block is the smallest 2^s, s >= -126, with |x| <= 448 * 2^s for all
+ * its finite numbers (2^0 if they are all zero or there are none); x * 2^-s is rounded to nearest, ties to even.  NaN
+ * and infinities become NaN.  Bytes from the end of a row to the next multiple of 16 are cleared; further ones are not touched.
+ */
+oz2_status oz2_f8_quantize(int64_t rows, int64_t cols, const void *X, int64_t ldx, oz2_type type, const oz2_f8 *as_is,
+                           const oz2_f8 *transposed, hipStream_t stream);
+
+/*
+ * C <- alpha * A * B^T + beta * C for A: m x k and B: n x k in 8 bits, C: m x n of `type` (ldc >= n).  With A = activations, B =
+ * a weight (outputs x inputs) this is a layer; with the transposed forms of oz2_f8_quantize the gradients of its input and
+ * of its weight.  beta == 0: C is not read.  k == 0: C <- beta * C, A and B may be NULL.
+ */
+oz2_status oz2_f8_gemm(int64_t m, int64_t n, int64_t k, float alpha, const oz2_f8 *A, const oz2_f8 *B, float beta, void *C,
+                       int64_t ldc, oz2_type type, hipStream_t stream);
+oz2_status oz2_ctx_f8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, float alpha, const oz2_f8 *A, const oz2_f8 *B,
+                           float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream);
+
+/*
+ * The gated feed-forward block up to its last projection: H = act(X Wg^T) * (X Wu^T), entry by entry, in one pass.  X: m x k in 8 bits,
+ * Wg and Wu: f x k, stored as one matrix W whose rows 0 .. f - 1 are Wg's and whose rows up .. up + f - 1 are Wu's, up = f
+ * rounded up to a multiple of 128; rows between are not read here, but oz2_f8_gemm on the whole of W reads them: keep them zero.
+ * H: m x f of `type` (ldh >= f).  Z (may be NULL): m x (up + f) of `type`, ldz >= up + f, receives X W^T, which
+ * oz2_f8_gated_grad needs (columns f .. up - 1 are not written); H comes from the sums before they are rounded.
+ */
+oz2_status oz2_f8_gated(int64_t m, int64_t f, int64_t k, oz2_act act, const oz2_f8 *X, const oz2_f8 *W, void *H, int64_t ldh,
+                        void *Z, int64_t ldz, oz2_type type, hipStream_t stream);
+oz2_status oz2_ctx_f8_gated(oz2_context *ctx, int64_t m, int64_t f, int64_t k, oz2_act act, const oz2_f8 *X, const oz2_f8 *W,
+                            void *H, int64_t ldh, void *Z, int64_t ldz, oz2_type type, hipStream_t stream);
+
+/*
+ * Its backward pass up to the products: from Z (as oz2_f8_gated wrote it) and dH (m x f, lddh >= f), both of `type`, the gradient of
+ * Z, (dH * Zu * act'(Zg), 0, dH * act(Zg)) of m x (up + f), computed in binary32 and written in 8 bits with blocks of one row: D as it
+ * is, DT transposed ((up + f) x m); one of them may be NULL.  Then dX = D * W is oz2_f8_gemm(m, k, up + f, D, W transposed) and
+ * dW = D^T * X is oz2_f8_gemm(up + f, k, m, DT, X transposed).
+ */
+oz2_status oz2_f8_gated_grad(int64_t m, int64_t f, oz2_act act, const void *Z, int64_t ldz, const void *dH, int64_t lddh,
+                             oz2_type type, const oz2_f8 *D, const oz2_f8 *DT, hipStream_t stream);
+
+/*
+ * Workspace of oz2_f8_gemm (gated = 0) and oz2_f8_gated (gated != 0, n = f): planes for the K ranges of a product with few tiles
+ * and a long contraction, 0 for all others.  The library's own workspace grows for them as for any product; a caller's buffer, or a
+ * limit, that has no room for them serves the call with one range (slower, and the sums in another order).
+ */
+size_t oz2_f8_workspace_bytes(int64_t m, int64_t n, int64_t k, int gated);
+
+/*
  * Constants of Section 4.1 for `num_moduli` moduli, written to HOST arrays of
  * at least num_moduli entries (any of them may be NULL):
  *   p           moduli p_i

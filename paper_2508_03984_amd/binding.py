@@ -30,11 +30,20 @@ EXPORTS = [
     "oz2_ctx_workspace_min_bytes", "oz2_ctx_set_workspace", "oz2_ctx_set_workspace_limit",
     "oz2_ctx_plan_panels", "oz2_ctx_last_panels", "oz2_ctx_release", "oz2_ctx_stage_ptr",
     "oz2_ctx_last_stage_times_ms", "oz2_dgemm_noalloc",
+    "oz2_f8_quantize", "oz2_f8_gemm", "oz2_f8_gated", "oz2_f8_gated_grad", "oz2_f8_workspace_bytes",
+    "oz2_ctx_f8_gemm", "oz2_ctx_f8_gated",
 ]
 
 OZ2_OPT_INT32_PRODUCTS, OZ2_OPT_OVERLAP, OZ2_OPT_SMALL_CONVERSION, OZ2_OPT_PROFILING, OZ2_OPT_CUT_LAUNCHES = range(5)
 
 OZ2_OP_N, OZ2_OP_T = 0, 1
+
+OZ2_BF16, OZ2_F16, OZ2_F32 = range(3)
+OZ2_ACT_SILU, OZ2_ACT_GELU = range(2)
+
+
+class _F8Struct(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ld", C.c_int64), ("scale", C.c_void_p), ("ld_scale", C.c_int64), ("block_rows", C.c_int)]
 
 
 class OZ2Error(RuntimeError):
@@ -128,6 +137,15 @@ def load():
     lib.oz2_ctx_release.argtypes = [vp]
     lib.oz2_ctx_stage_ptr.argtypes = [vp] + lib.oz2_stage_ptr.argtypes
     lib.oz2_ctx_last_stage_times_ms.argtypes = [vp, C.POINTER(flt)]
+    f8 = C.POINTER(_F8Struct)
+    lib.oz2_f8_quantize.argtypes = [i64, i64, vp, i64, ci, f8, f8, vp]
+    lib.oz2_f8_gemm.argtypes = [i64, i64, i64, flt, f8, f8, flt, vp, i64, ci, vp]
+    lib.oz2_ctx_f8_gemm.argtypes = [vp] + lib.oz2_f8_gemm.argtypes
+    lib.oz2_f8_gated.argtypes = [i64, i64, i64, ci, f8, f8, vp, i64, vp, i64, ci, vp]
+    lib.oz2_ctx_f8_gated.argtypes = [vp] + lib.oz2_f8_gated.argtypes
+    lib.oz2_f8_gated_grad.argtypes = [i64, i64, ci, vp, i64, vp, i64, ci, f8, f8, vp]
+    lib.oz2_f8_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    lib.oz2_f8_workspace_bytes.restype = C.c_size_t
     for name in EXPORTS:
         if name.startswith("oz2_ctx_") or name in ("oz2_create", "oz2_destroy"):
             getattr(lib, name).restype = ci
@@ -142,7 +160,7 @@ def load():
                  "oz2_stage_ptr", "oz2_int8_gemm", "oz2_last_stage_times_ms", "oz2_mfma_probe",
                  "oz2_dgemm_op", "oz2_sgemm_op", "oz2_prepare_d", "oz2_prepare_s", "oz2_dgemm_prepared",
                  "oz2_sgemm_prepared", "oz2_last_panels", "oz2_plan_panels", "oz2_dgemm_colmajor",
-                 "oz2_sgemm_colmajor"):
+                 "oz2_sgemm_colmajor", "oz2_f8_quantize", "oz2_f8_gemm", "oz2_f8_gated", "oz2_f8_gated_grad"):
         getattr(lib, name).restype = ci
     _lib = lib
     return lib
@@ -578,6 +596,119 @@ def oz2_ctx_last_stage_times_ms(ctx):
     out = (C.c_float * 4)()
     _check(load().oz2_ctx_last_stage_times_ms(_ctx(ctx), out), "oz2_ctx_last_stage_times_ms")
     return [float(x) for x in out]
+
+
+# ------------------------------------------------------------------ 8-bit floating point
+def _up(x: int, to: int) -> int:
+    return -(-x // to) * to
+
+
+class F8:
+    """A rows x cols matrix in 8 bits on the device (oz2_f8): `q`, E4M3 numbers (torch.float8_e4m3fn), and `scale`, the powers of
+    two of its blocks (torch.float8_e8m0fnu), of `block_rows` (1 or 128) x 128 elements.  Keep it as long as the tensors' memory: a call reads
+    the addresses from here."""
+
+    __slots__ = ("q", "scale", "block_rows", "ref", "_struct")
+
+    def __init__(self, q, scale, block_rows: int):
+        torch = _th()
+        rows, cols = q.shape
+        if q.dtype is not torch.float8_e4m3fn or scale.dtype is not torch.float8_e8m0fnu:
+            raise ValueError("q of dtype float8_e4m3fn and scale of dtype float8_e8m0fnu expected")
+        if block_rows not in (1, 128) or tuple(scale.shape) != (-(-rows // block_rows), -(-cols // 128)):
+            raise ValueError(f"scale of {-(-rows // block_rows)} x {-(-cols // 128)} blocks expected, got {tuple(scale.shape)}")
+        if (cols > 1 and q.stride(1) != 1) or (scale.shape[1] > 1 and scale.stride(1) != 1):
+            raise ValueError("row-major q and scale expected")
+        ld = q.stride(0) if rows > 1 else max(q.stride(0), _up(cols, 16))
+        ld_scale = scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), _up(scale.shape[1], 4))
+        for t, row, unit in ((q, cols, 16), (scale, scale.shape[1], 4)):        # the last row is stored whole, too
+            left = t.untyped_storage().nbytes() - t.storage_offset() - (t.shape[0] - 1) * t.stride(0)
+            if t.numel() and left < _up(row, unit):
+                raise ValueError(f"rows have to be stored up to the next multiple of {unit} bytes")
+        self.q, self.scale, self.block_rows = q, scale, block_rows
+        self._struct = _F8Struct(_dev(q), ld, _dev(scale), ld_scale, block_rows)
+        self.ref = C.byref(self._struct)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block_rows: int = 1, device="cuda") -> "F8":
+        """Memory for rows x cols elements, with rows on multiples of 128 bytes."""
+        torch = _th()
+        blocks = -(-cols // 128)
+        q = torch.empty((rows, max(_up(cols, 128), 128)), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        scale = torch.empty((-(-rows // block_rows), max(_up(blocks, 4), 4)), dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
+        return cls(q[:, :cols], scale[:, :blocks], block_rows)
+
+    @classmethod
+    def of(cls, q, scale, block_rows: int = 1) -> "F8":
+        """A copy of q and scale, which may have any strides, where their rows are stored as the products need them."""
+        out = cls.empty(q.shape[0], q.shape[1], block_rows, q.device)
+        out.q.copy_(q)
+        out.scale.copy_(scale)
+        return out
+
+    @property
+    def shape(self):
+        return tuple(self.q.shape)
+
+
+_f8_types = None
+
+
+def _f8_type(t) -> int:
+    global _f8_types
+    if _f8_types is None:
+        torch = _th()
+        _f8_types = {torch.bfloat16: OZ2_BF16, torch.float16: OZ2_F16, torch.float32: OZ2_F32}
+    if t.dtype not in _f8_types:
+        raise ValueError(f"tensor of dtype bfloat16, float16 or float32 expected, got {t.dtype}")
+    return _f8_types[t.dtype]
+
+
+def _f8_ref(x, rows: int, cols: int):
+    """The struct of a matrix that has at least rows x cols elements; None for None."""
+    if x is None:
+        return None
+    if x.q.shape[0] < rows or x.q.shape[1] < cols:
+        raise ValueError(f"matrix of {rows} x {cols} elements in 8 bits expected, got {x.q.shape[0]} x {x.q.shape[1]}")
+    return x.ref
+
+
+def oz2_f8_quantize(rows, cols, X, ldx, as_is, transposed, stream=None) -> None:
+    _check(load().oz2_f8_quantize(rows, cols, _dev(X), ldx, _f8_type(X), _f8_ref(as_is, rows, cols),
+                                  _f8_ref(transposed, cols, rows), _stream(stream)), "oz2_f8_quantize")
+
+
+def oz2_ctx_f8_gemm(ctx, m, n, k, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    _check(load().oz2_ctx_f8_gemm(_ctx(ctx), m, n, k, alpha, _f8_ref(A, m, k), _f8_ref(B, n, k), beta, _dev(C_), ldc,
+                                  _f8_type(C_), _stream(stream)), "oz2_ctx_f8_gemm")
+
+
+def oz2_f8_gemm(m, n, k, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    _check(load().oz2_f8_gemm(m, n, k, alpha, _f8_ref(A, m, k), _f8_ref(B, n, k), beta, _dev(C_), ldc, _f8_type(C_),
+                              _stream(stream)), "oz2_f8_gemm")
+
+
+def _gated_args(m, f, k, act, X, W, H, ldh, Z, ldz, stream):
+    return (m, f, k, act, _f8_ref(X, m, k), _f8_ref(W, _up(f, 128) + f, k), _dev(H), ldh, _dev(Z, H.dtype), ldz, _f8_type(H),
+            _stream(stream))
+
+
+def oz2_ctx_f8_gated(ctx, m, f, k, act, X, W, H, ldh, Z=None, ldz=0, stream=None) -> None:
+    _check(load().oz2_ctx_f8_gated(_ctx(ctx), *_gated_args(m, f, k, act, X, W, H, ldh, Z, ldz, stream)), "oz2_ctx_f8_gated")
+
+
+def oz2_f8_gated(m, f, k, act, X, W, H, ldh, Z=None, ldz=0, stream=None) -> None:
+    _check(load().oz2_f8_gated(*_gated_args(m, f, k, act, X, W, H, ldh, Z, ldz, stream)), "oz2_f8_gated")
+
+
+def oz2_f8_gated_grad(m, f, act, Z, ldz, dH, lddh, D, DT, stream=None) -> None:
+    wide = _up(f, 128) + f
+    _check(load().oz2_f8_gated_grad(m, f, act, _dev(Z), ldz, _dev(dH, Z.dtype), lddh, _f8_type(Z), _f8_ref(D, m, wide),
+                                    _f8_ref(DT, wide, m), _stream(stream)), "oz2_f8_gated_grad")
+
+
+def oz2_f8_workspace_bytes(m, n, k, gated=False) -> int:
+    return int(load().oz2_f8_workspace_bytes(m, n, k, int(bool(gated))))
 
 
 # ------------------------------------------------------------------ conveniences (no arithmetic)

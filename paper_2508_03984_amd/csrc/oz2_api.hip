@@ -12,6 +12,7 @@
 
 #include "../../include/oz2.h"
 #include "oz2_constants.hpp"
+#include "oz2_f8.hpp"
 #include "oz2_kernels.hpp"
 #include "oz2_plan.hpp"
 
@@ -914,6 +915,156 @@ const char *oz2_status_string(oz2_status s) {
     case OZ2_HIP_ERROR: return "HIP runtime error";
     }
     return "unknown status";
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ 8-bit floating point
+namespace {
+
+constexpr int64_t kF8MaxRows = (int64_t)1 << 30, kF8MaxLd = (int64_t)1 << 23;
+
+// What the kernels rely on, for `rows` rows of k elements; *out is written if it holds.
+oz2_status f8_matrix(const oz2_f8 *x, int64_t k, F8Matrix *out) {
+    if (!x || !x->q || !x->scale || (x->block_rows != 1 && x->block_rows != kF8Block)) return OZ2_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(x->q) % 16 || x->ld % 16 || x->ld < k) return OZ2_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(x->scale) % 4 || x->ld_scale % 4 || x->ld_scale < f8_blocks(k)) return OZ2_INVALID_ARG;
+    if (x->ld > kF8MaxLd || x->ld_scale > kF8MaxLd) return OZ2_UNSUPPORTED;
+    *out = F8Matrix{static_cast<const uint8_t *>(x->q), x->ld, static_cast<const uint8_t *>(x->scale), x->ld_scale, x->block_rows == 1 ? 0 : 7};
+    return OZ2_OK;
+}
+
+oz2_status f8_target(const oz2_f8 *x, int64_t k, F8Target *out) {
+    F8Matrix checked;
+    *out = F8Target{nullptr, 0, nullptr, 0};
+    if (!x) return OZ2_OK;
+    if (oz2_status st = f8_matrix(x, k, &checked)) return st;
+    *out = F8Target{static_cast<uint8_t *>(x->q), x->ld, static_cast<uint8_t *>(x->scale), x->ld_scale};
+    return OZ2_OK;
+}
+
+bool f8_type_ok(int type) { return type == kF8Bf16 || type == kF8F16 || type == kF8F32; }
+// A matrix of numbers of `type` with `cols` columns.
+bool f8_numbers_ok(const void *p, int64_t ld, int64_t cols, int type) {
+    return p && ld >= cols && reinterpret_cast<uintptr_t>(p) % f8_type_bytes(type) == 0;
+}
+int f8_vec(const void *p, int64_t ld, int type) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * f8_type_bytes(type) % 16 == 0; }
+
+// m, n (columns of C), k of a product; kNothing: there is nothing to do.
+oz2_status f8_sizes(int64_t m, int64_t n, int64_t k, int type, bool *nothing) {
+    if (m < 0 || n < 0 || k < 0 || !f8_type_ok(type)) return OZ2_INVALID_ARG;
+    *nothing = m == 0 || n == 0;
+    if (m > kF8MaxRows || n > kF8MaxRows || k > OZ2_MAX_K_BLOCKED || f8_tiles(m, 2 * n, 128) >= kF8MaxRows) return OZ2_UNSUPPORTED;
+    return OZ2_OK;
+}
+
+oz2_status f8_run(Ctx &g, F8Args &args, bool gated, hipStream_t stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    F8Plan plan = f8_plan(args.m, args.n, args.k, gated);
+    if (plan.ranges > 1) {
+        size_t have = 0, with_planes = 0;
+        if (ensure_workspace(g, plan.plane_bytes, 0, &have, &with_planes) == OZ2_OK && with_planes >= plan.plane_bytes && g.ws) {
+            g.have_last = g.have_last_prod = false;            // the stages of the product before are overwritten
+            args.out.planes = reinterpret_cast<float *>(g.ws);
+            args.out.ldp = f8_plane_ld(args.n, gated);
+            args.out.plane = (int64_t)args.m * args.out.ldp;
+        } else {
+            plan.ranges = 1;
+            plan.kb_each = (int)f8_blocks(args.k);
+        }
+    }
+    args.ranges = plan.ranges;
+    args.kb_each = plan.kb_each;
+    OZ2_TRY(launch_f8_product(args, plan, gated, stream));
+    return OZ2_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+oz2_status oz2_f8_quantize(int64_t rows, int64_t cols, const void *X, int64_t ldx, oz2_type type, const oz2_f8 *as_is,
+                           const oz2_f8 *transposed, hipStream_t stream) {
+    if (rows < 0 || cols < 0 || !f8_type_ok(type) || (!as_is && !transposed)) return OZ2_INVALID_ARG;
+    if (rows == 0 || cols == 0) return OZ2_OK;
+    if (!f8_numbers_ok(X, ldx, cols, type)) return OZ2_INVALID_ARG;
+    if (as_is && transposed && as_is->block_rows != transposed->block_rows) return OZ2_INVALID_ARG;
+    F8Target out, turned;
+    if (oz2_status st = f8_target(as_is, cols, &out)) return st;
+    if (oz2_status st = f8_target(transposed, rows, &turned)) return st;
+    if (rows > kF8MaxRows || cols > kF8MaxRows || rows * f8_blocks(cols) >= kF8MaxRows) return OZ2_UNSUPPORTED;
+    const bool square = (as_is ? as_is : transposed)->block_rows != 1;
+    OZ2_TRY(launch_f8_quantize(X, type, rows, cols, ldx, square, out, turned, stream));
+    return OZ2_OK;
+}
+
+oz2_status oz2_ctx_f8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, float alpha, const oz2_f8 *A, const oz2_f8 *B,
+                           float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
+    bool nothing = false;
+    if (oz2_status st = f8_sizes(m, n, k, type, &nothing)) return st;
+    if (nothing) return OZ2_OK;
+    if (!f8_numbers_ok(C, ldc, n, type)) return OZ2_INVALID_ARG;
+    F8Args args{};
+    if (k > 0) {
+        if (oz2_status st = f8_matrix(A, k, &args.A)) return st;
+        if (oz2_status st = f8_matrix(B, k, &args.B)) return st;
+    }
+    args.m = (int)m; args.n = (int)n; args.k = (int)k;
+    args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.vec = f8_vec(C, ldc, type);
+    args.out.alpha = alpha; args.out.beta = beta;
+    return f8_run(resolve(ctx), args, false, stream);
+}
+
+oz2_status oz2_f8_gemm(int64_t m, int64_t n, int64_t k, float alpha, const oz2_f8 *A, const oz2_f8 *B, float beta, void *C,
+                       int64_t ldc, oz2_type type, hipStream_t stream) {
+    return oz2_ctx_f8_gemm(nullptr, m, n, k, alpha, A, B, beta, C, ldc, type, stream);
+}
+
+oz2_status oz2_ctx_f8_gated(oz2_context *ctx, int64_t m, int64_t f, int64_t k, oz2_act act, const oz2_f8 *X, const oz2_f8 *W,
+                            void *H, int64_t ldh, void *Z, int64_t ldz, oz2_type type, hipStream_t stream) {
+    bool nothing = false;
+    if (oz2_status st = f8_sizes(m, f, k, type, &nothing)) return st;
+    if (act != OZ2_ACT_SILU && act != OZ2_ACT_GELU) return OZ2_INVALID_ARG;
+    if (nothing) return OZ2_OK;
+    const int64_t up = f8_blocks(f) * kF8Block;
+    if (!f8_numbers_ok(H, ldh, f, type) || (Z && !f8_numbers_ok(Z, ldz, up + f, type))) return OZ2_INVALID_ARG;
+    F8Args args{};
+    if (k > 0) {
+        if (oz2_status st = f8_matrix(X, k, &args.A)) return st;
+        if (oz2_status st = f8_matrix(W, k, &args.B)) return st;
+    }
+    args.m = (int)m; args.n = (int)f; args.k = (int)k; args.up = (int)up;
+    args.out.C = H; args.out.ldc = ldh; args.out.type = type; args.out.vec = f8_vec(H, ldh, type);
+    args.out.alpha = 1.0f; args.out.act = act;
+    args.out.Z = Z; args.out.ldz = ldz; args.out.z_vec = Z && f8_vec(Z, ldz, type);
+    return f8_run(resolve(ctx), args, true, stream);
+}
+
+oz2_status oz2_f8_gated(int64_t m, int64_t f, int64_t k, oz2_act act, const oz2_f8 *X, const oz2_f8 *W, void *H, int64_t ldh,
+                        void *Z, int64_t ldz, oz2_type type, hipStream_t stream) {
+    return oz2_ctx_f8_gated(nullptr, m, f, k, act, X, W, H, ldh, Z, ldz, type, stream);
+}
+
+oz2_status oz2_f8_gated_grad(int64_t m, int64_t f, oz2_act act, const void *Z, int64_t ldz, const void *dH, int64_t lddh,
+                             oz2_type type, const oz2_f8 *D, const oz2_f8 *DT, hipStream_t stream) {
+    bool nothing = false;
+    if (oz2_status st = f8_sizes(m, f, 0, type, &nothing)) return st;
+    if ((act != OZ2_ACT_SILU && act != OZ2_ACT_GELU) || (!D && !DT)) return OZ2_INVALID_ARG;
+    if (nothing) return OZ2_OK;
+    const int64_t up = f8_blocks(f) * kF8Block;
+    if (!f8_numbers_ok(Z, ldz, up + f, type) || !f8_numbers_ok(dH, lddh, f, type)) return OZ2_INVALID_ARG;
+    if ((D && D->block_rows != 1) || (DT && DT->block_rows != 1)) return OZ2_INVALID_ARG;
+    F8Target d, dt;
+    if (oz2_status st = f8_target(D, up + f, &d)) return st;
+    if (oz2_status st = f8_target(DT, m, &dt)) return st;
+    OZ2_TRY(launch_f8_gated_grad(Z, ldz, dH, lddh, type, m, f, up, act, d, dt, stream));
+    return OZ2_OK;
+}
+
+size_t oz2_f8_workspace_bytes(int64_t m, int64_t n, int64_t k, int gated) {
+    bool nothing = false;
+    if (f8_sizes(m, n, k, kF8Bf16, &nothing) || nothing) return 0;
+    return f8_plan(m, n, k, gated != 0).plane_bytes;
 }
 
 }  // extern "C"

@@ -1,0 +1,123 @@
+// Device code shared by the kernels of 8-bit floating-point products.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "oz2_f8.hpp"
+
+namespace oz2 {
+
+typedef int f8_v4i __attribute__((ext_vector_type(4)));
+typedef int f8_v8i __attribute__((ext_vector_type(8)));
+typedef float f8_v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 f8_bf2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f8_h2 __attribute__((ext_vector_type(2)));
+typedef float f8_f2 __attribute__((ext_vector_type(2)));
+
+// acc + sum over 128 of b * a, scaled by 2^(byte 0 of sb - 127) 2^(byte 0 of sa - 127).  Lane l holds of row l % 16 of either factor
+// the 32 elements of quarter l / 16 (in the same order for both) and that row's scale; of the result, row 4 (l / 16) + r of b and
+// column l % 16, a row of a.
+__device__ __forceinline__ f8_v4f f8_mfma(const f8_v8i &b, const f8_v8i &a, const f8_v4f &acc, int sb, int sa) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, 0, 0, 0, sb, 0, sa);
+}
+__device__ __forceinline__ f8_v8i f8_join(const f8_v4i &lo, const f8_v4i &hi) {
+    return f8_v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+}
+// The first `valid` (at most 16) of 16 bytes, zeros behind them.
+__device__ __forceinline__ f8_v4i f8_keep(f8_v4i v, int valid) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int bytes = valid - 4 * w;
+        if (bytes < 4) v[w] = bytes <= 0 ? 0 : v[w] & ((1 << 8 * bytes) - 1);
+    }
+    return v;
+}
+
+// Both activations are g / (1 + exp(-s)): s = g (SiLU), s = 2 sqrt(2 / pi) (g + 0.044715 g^3) (GELU, tanh form, since
+// (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))).  Their slope is p + g p (1 - p) s' with p = 1 / (1 + exp(-s)).
+constexpr float kGeluScale = 1.5957691216057308f, kGeluCube = 0.044715f;
+__device__ __forceinline__ float f8_gate(float g, int act) {
+    const float s = act ? kGeluScale * __builtin_fmaf(kGeluCube * g * g, g, g) : g;
+    return 1.0f / (1.0f + expf(-s));
+}
+__device__ __forceinline__ float f8_act(float g, int act) { return g * f8_gate(g, act); }
+__device__ __forceinline__ float f8_slope(float g, float p, int act) {
+    const float ds = act ? kGeluScale * __builtin_fmaf(3.0f * kGeluCube * g, g, 1.0f) : 1.0f, q = p * (1.0f - p);
+    return q > 0.0f ? __builtin_fmaf(g * q, ds, p) : p;         // p is 0 or 1 (or NaN): the slope's limit, also where s' overflows
+}
+
+// Numbers of one type from and to binary32, rounded to nearest even.
+template <int TYPE>
+struct F8Number;
+template <>
+struct F8Number<kF8Bf16> {
+    typedef uint16_t T;
+    static __device__ __forceinline__ float get(T x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f8_f2){x, y}, f8_bf2)); }
+};
+template <>
+struct F8Number<kF8F16> {
+    typedef uint16_t T;
+    static __device__ __forceinline__ float get(T x) { return (float)__builtin_bit_cast(_Float16, x); }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f8_f2){x, y}, f8_h2)); }
+};
+template <>
+struct F8Number<kF8F32> {
+    typedef float T;
+    static __device__ __forceinline__ float get(T x) { return x; }
+};
+
+__device__ __forceinline__ float f8_load(const void *C, int type, int64_t at) {
+    return type == kF8Bf16 ? F8Number<kF8Bf16>::get(static_cast<const uint16_t *>(C)[at])
+         : type == kF8F16  ? F8Number<kF8F16>::get(static_cast<const uint16_t *>(C)[at])
+                           : static_cast<const float *>(C)[at];
+}
+__device__ __forceinline__ void f8_store(void *C, int type, int64_t at, float x) {
+    if (type == kF8Bf16) static_cast<uint16_t *>(C)[at] = (uint16_t)F8Number<kF8Bf16>::pack(x, x);
+    else if (type == kF8F16) static_cast<uint16_t *>(C)[at] = (uint16_t)F8Number<kF8F16>::pack(x, x);
+    else static_cast<float *>(C)[at] = x;
+}
+
+// N (a multiple of 4) numbers in a row from C[at] on, of which `valid` exist; vec: C + at is on a multiple of N bytes, at most 16.
+template <int N>
+__device__ __forceinline__ void f8_store_row(void *C, int type, int64_t at, const float (&x)[N], int valid, bool vec) {
+    if (!vec || valid < N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < valid) f8_store(C, type, at + i, x[i]);
+        return;
+    }
+    if (type == kF8F32) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<f8_v4f *>(static_cast<float *>(C) + at + i) = f8_v4f{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        return;
+    }
+    uint32_t w[N / 2];
+    if (type == kF8Bf16) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) w[i] = F8Number<kF8Bf16>::pack(x[2 * i], x[2 * i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) w[i] = F8Number<kF8F16>::pack(x[2 * i], x[2 * i + 1]);
+    }
+    uint16_t *const to = static_cast<uint16_t *>(C) + at;
+    if constexpr (N == 4) {
+        *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i)
+            reinterpret_cast<f8_v4i *>(to)[i] = f8_v4i{(int)w[4 * i], (int)w[4 * i + 1], (int)w[4 * i + 2], (int)w[4 * i + 3]};
+    }
+}
+
+// alpha * x + beta * C, and its store.
+template <int N>
+__device__ __forceinline__ void f8_update_row(const F8Out &o, int64_t at, float (&x)[N], int valid, bool vec) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] *= o.alpha;
+        if (o.beta != 0.0f && i < valid) x[i] = __builtin_fmaf(o.beta, f8_load(o.C, o.type, at + i), x[i]);
+    }
+    f8_store_row<N>(o.C, o.type, at, x, valid, vec);
+}
+
+}  // namespace oz2

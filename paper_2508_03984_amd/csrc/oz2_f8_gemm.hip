@@ -1,0 +1,256 @@
+// Products of E4M3 matrices with a power of two per block of 128, C = A B^T, by tiles of C, and the gated block on the same core.
+//
+// sum_h a_ih b_jh = sum over blocks of 2^(sa + sb) sum within the block: v_mfma_scale_f32_16x16x128_f8f6f4 takes one block of 128 of
+// 16 rows by 16 columns with both scales as E8M0 bytes, so the sums stay in its binary32 accumulators from the first block to the last.
+// The matrix core aligns the products of 8 consecutive k to the largest of them and cuts them towards zero at 2^-13 of it (measured;
+// 1.4e-5 of the norm of the result for normal data, the same for the instructions with k = 32 and 64), then adds groups and accumulator in
+// binary32; the E4M3 numbers themselves are rounded at 2^-4.
+//
+// Rows of A and B lie as the caller has them.  A stage of LDS holds the 128 bytes of a block of every row of the tile; the 16-byte
+// chunk c of row r is at place c ^ (r / 2 % 8), which gives every 16 lanes that LDS serves together 16 different places (two rows
+// cover all banks).  Rows beyond the matrix are read as its last one and their results dropped; in the last block, chunks
+// beyond k are read as the row's last one and then cleared in LDS, in both factors, since 0 times what lies there may be NaN.
+#include "oz2_epilogue.hpp"
+#include "oz2_f8_device.hpp"
+
+namespace oz2 {
+namespace {
+
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
+
+__device__ __forceinline__ void wait_all_and_meet() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+extern __shared__ f8_v4i f8_lds[];
+
+// WM x WN wavefronts with FM x FN blocks of 16 x 16 each.  GATED: the columns of a wavefront's blocks j < FN / 2 come from the first
+// weight, those of block j + FN / 2 are the same columns of the second one.
+template <int WM, int WN, int FM, int FN, bool GATED>
+struct F8Core {
+    static constexpr int WAVES = WM * WN, THREADS = WAVES * 64;
+    static constexpr int BM = WM * FM * 16, BN = WN * FN * 16;            // rows of A and of B in a stage
+    static constexpr int ROWS = BM + BN, STAGE_BYTES = ROWS * 128;
+    static constexpr int LOADS = ROWS / 8 / WAVES, A_LOADS = BM / 8 / WAVES;
+    static constexpr int COLS = GATED ? BN / 2 : BN, FC = GATED ? FN / 2 : FN;   // columns of C of a tile; blocks of a wavefront
+    static constexpr size_t LDS_BYTES = 2 * STAGE_BYTES + 2 * ROWS * 4;
+    static_assert(ROWS == THREADS && WAVES % 2 == 0 && BM % (8 * WAVES) == 0, "");
+};
+
+template <int WM, int WN, int FM, int FN, bool GATED>
+__global__ __launch_bounds__(WM *WN * 64, 2) void k_f8_tiles(F8Args p, TileMap map) {
+    typedef F8Core<WM, WN, FM, FN, GATED> C;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN, lrow = lane & 15, quarter = lane >> 4;
+    int range, tr, tc;
+    map_tile(map, (int)blockIdx.x, range, tr, tc);
+    const int row0 = tr * C::BM, col0 = tc * C::COLS;
+    const int rows = min(C::BM, p.m - row0), cols = min(C::COLS, p.n - col0);
+    const int KB = (p.k + kF8Block - 1) / kF8Block, kb0 = range * p.kb_each, kb1 = min(kb0 + p.kb_each, KB);
+
+    // Row of B for row r of that part of a stage: the column of C and, gated, which of the two weights.
+    const auto b_column = [](int r) { return GATED ? r / (FN * 16) * (FN * 8) + r % (FN * 8) : r; };
+    const auto b_second = [](int r) { return GATED && r / (FN * 8) % 2; };
+
+    // Load H of this wavefront takes the 8 rows from 8 (H WAVES + wave) on; a lane 16 bytes of one.
+    const uint8_t *const a_base = p.A.q + (int64_t)row0 * p.A.ld, *const b_base = p.B.q + (int64_t)col0 * p.B.ld;
+    const uint8_t *const b_base2 = GATED ? b_base + (int64_t)p.up * p.B.ld : b_base;
+    const int chunk = (lane & 7) ^ ((wave & 1) * 4 + quarter);
+    uint32_t offset[C::LOADS];
+#pragma unroll
+    for (int h = 0; h < C::LOADS; ++h) {
+        const int r = (h * C::WAVES + wave) * 8 + (lane >> 3);
+        offset[h] = h < C::A_LOADS ? (uint32_t)min(r, rows - 1) * (uint32_t)p.A.ld : (uint32_t)min(b_column(r - C::BM), cols - 1) * (uint32_t)p.B.ld;
+        offset[h] += chunk * 16;
+    }
+    const int in_last = p.k - (KB - 1) * kF8Block;                         // of the last block, 1 to 128
+    const int to_last_chunk = (min(chunk, (in_last - 1) / 16) - chunk) * 16;
+    // A lane's scales: four blocks of one row, those of all rows are fetched by the workgroup together.
+    const uint8_t *scales;
+    {
+        const int r = (int)threadIdx.x;
+        if (r < C::BM) scales = p.A.scale + (int64_t)((row0 + min(r, rows - 1)) >> p.A.shift) * p.A.ld_scale;
+        else {
+            const int br = col0 + min(b_column(r - C::BM), cols - 1) + (b_second(r - C::BM) ? p.up : 0);
+            scales = p.B.scale + (int64_t)(br >> p.B.shift) * p.B.ld_scale;
+        }
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)f8_lds;
+    const auto request = [&](int kb, int stage) {
+        const uint32_t back = kb == KB - 1 ? (uint32_t)to_last_chunk : 0u;
+#pragma unroll
+        for (int h = 0; h < C::LOADS; ++h) {
+            const bool second = h >= C::A_LOADS && b_second((h * C::WAVES + wave) * 8 - C::BM);       // uniform
+            const uint8_t *const base = (h < C::A_LOADS ? a_base : second ? b_base2 : b_base) + (int64_t)kb * kF8Block;
+            const uint32_t to = lds0 + stage * C::STAGE_BYTES + (h * C::WAVES + wave) * 1024;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset[h] + back), "s"(base) : "memory");
+        }
+        if ((kb & 3) == 0) {
+            const uint32_t to = lds0 + 2 * C::STAGE_BYTES + ((kb >> 2 & 1) * C::ROWS + wave * 64) * 4;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(scales + kb) : "memory");
+        }
+    };
+
+    f8_v4f acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f8_v4f{0.f, 0.f, 0.f, 0.f};
+    int sa[FM], sb[FN];
+    const char *const lds = reinterpret_cast<const char *>(f8_lds);
+    const int swizzled = (quarter ^ (lane >> 1 & 7)) * 16;
+    const int a_addr = (wm * FM * 16 + lrow) * 128 + swizzled, b_addr = (C::BM + wn * FN * 16 + lrow) * 128 + swizzled;
+
+    if (kb0 < kb1) request(kb0, 0);
+    for (int kb = kb0; kb < kb1; ++kb) {
+        const int stage = (kb - kb0) & 1;
+        wait_all_and_meet();                                               // block kb is there, and nobody reads the other stage
+        if (kb + 1 < kb1) request(kb + 1, stage ^ 1);
+        if (kb == KB - 1 && in_last < kF8Block) {
+            const int r = (int)threadIdx.x;
+            f8_v4i *const row = f8_lds + stage * (C::STAGE_BYTES / 16) + r * 8;
+            const int from = in_last >> 4, f = r >> 1 & 7;
+            row[from ^ f] = f8_keep(row[from ^ f], in_last & 15);
+            for (int c = from + 1; c < 8; ++c) row[c ^ f] = f8_v4i{0, 0, 0, 0};
+            wait_all_and_meet();
+        }
+        if ((kb & 3) == 0) {
+            const int *const s = reinterpret_cast<const int *>(lds + 2 * C::STAGE_BYTES) + (kb >> 2 & 1) * C::ROWS;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) sa[i] = s[(wm * FM + i) * 16 + lrow];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) sb[j] = s[C::BM + (wn * FN + j) * 16 + lrow];
+        }
+        const char *const at = lds + stage * C::STAGE_BYTES;
+        f8_v8i a[FM];
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            a[i] = f8_join(*reinterpret_cast<const f8_v4i *>(at + a_addr + i * 2048), *reinterpret_cast<const f8_v4i *>(at + (a_addr ^ 64) + i * 2048));
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const f8_v8i b = f8_join(*reinterpret_cast<const f8_v4i *>(at + b_addr + j * 2048), *reinterpret_cast<const f8_v4i *>(at + (b_addr ^ 64) + j * 2048));
+#pragma unroll
+            for (int i = 0; i < FM; ++i) acc[i][j] = f8_mfma(b, a[i], acc[i][j], sb[j], sa[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = (int)((uint32_t)sa[i] >> 8);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sb[j] = (int)((uint32_t)sb[j] >> 8);
+    }
+
+    // Four blocks at a time, exchanged so that quarter q of the wavefront has 16 columns of block q's rows.
+    const auto gathered = [&](const f8_v4f &b0, const f8_v4f &b1, const f8_v4f &b2, const f8_v4f &b3, float(&x)[16]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float f[4] = {b0[r], b1[r], b2[r], b3[r]};               // (a bit cast of an element of a vector takes the first one)
+            const uint32_t d[4] = {__builtin_bit_cast(uint32_t, f[0]), __builtin_bit_cast(uint32_t, f[1]), __builtin_bit_cast(uint32_t, f[2]),
+                                   __builtin_bit_cast(uint32_t, f[3])};
+            const exchanged_t e = exchange_quarters(d);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int w = e[q];
+                x[4 * q + r] = __builtin_bit_cast(float, w);
+            }
+        }
+    };
+    // The four blocks are (i, j) to (i, j + 3), or, of two columns of blocks, (i, 0), (i, 1), (i + 1, 0), (i + 1, 1).
+    constexpr int GI = C::FC >= 4 ? 1 : 2, GJ = 4 / GI;
+    static_assert(FM % GI == 0 && C::FC % GJ == 0, "");
+    const F8Out &o = p.out;
+#pragma unroll
+    for (int i = 0; i < FM; i += GI)
+#pragma unroll
+        for (int j = 0; j < C::FC; j += GJ) {
+            const int row = row0 + (wm * FM + i + quarter / GJ) * 16 + lrow, col = col0 + (wn * C::FC + j + quarter % GJ) * 16;
+            const int valid = row < p.m ? p.n - col : 0;
+            const int i1 = i + (GI - 1), j1 = j + 1, j2 = GJ == 4 ? j + 2 : j, j3 = GJ == 4 ? j + 3 : j + 1;
+            float x[16];
+            gathered(acc[i][j], acc[i][j1], acc[i1][j2], acc[i1][j3], x);
+            if constexpr (!GATED) {
+                if (valid <= 0) continue;
+                if (o.planes) f8_store_row<16>(o.planes, kF8F32, range * o.plane + (int64_t)row * o.ldp + col, x, valid, true);
+                else f8_update_row<16>(o, (int64_t)row * o.ldc + col, x, valid, o.vec);
+            } else {
+                float u[16];
+                gathered(acc[i][j + C::FC], acc[i][j1 + C::FC], acc[i1][j2 + C::FC], acc[i1][j3 + C::FC], u);
+                if (valid <= 0) continue;
+                if (o.planes) {
+                    const int64_t at = range * o.plane + (int64_t)row * o.ldp + col;
+                    f8_store_row<16>(o.planes, kF8F32, at, x, valid, true);
+                    f8_store_row<16>(o.planes, kF8F32, at + o.ldp / 2, u, valid, true);
+                    continue;
+                }
+                if (o.Z) {
+                    f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + col, x, valid, o.z_vec);
+                    f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + p.up + col, u, valid, o.z_vec);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = f8_act(x[e], o.act) * u[e];
+                f8_store_row<16>(o.C, o.type, (int64_t)row * o.ldc + col, x, valid, o.vec);
+            }
+        }
+}
+
+// The sums of the K ranges, in ascending order, and what the tiles do with a sum.  A thread has 4 columns of a row.
+template <bool GATED>
+__global__ __launch_bounds__(256) void k_f8_ranges(F8Args p) {
+    const int per_row = (p.n + 3) / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / per_row;
+    if (row >= p.m) return;
+    const int col = (int)(id - row * per_row) * 4, valid = p.n - col;
+    const F8Out &o = p.out;
+    const float *from = o.planes + row * o.ldp + col;
+    f8_v4f s{0.f, 0.f, 0.f, 0.f}, t{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < p.ranges; ++r, from += o.plane) {
+        s += *reinterpret_cast<const f8_v4f *>(from);
+        if (GATED) t += *reinterpret_cast<const f8_v4f *>(from + o.ldp / 2);
+    }
+    float x[4] = {s[0], s[1], s[2], s[3]};
+    if constexpr (!GATED) f8_update_row<4>(o, row * o.ldc + col, x, valid, o.vec);
+    else {
+        float u[4] = {t[0], t[1], t[2], t[3]};
+        if (o.Z) {
+            f8_store_row<4>(o.Z, o.type, row * o.ldz + col, x, valid, o.z_vec);
+            f8_store_row<4>(o.Z, o.type, row * o.ldz + p.up + col, u, valid, o.z_vec);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = f8_act(x[e], o.act) * u[e];
+        f8_store_row<4>(o.C, o.type, row * o.ldc + col, x, valid, o.vec);
+    }
+}
+
+template <int WM, int WN, int FM, int FN, bool GATED>
+hipError_t launch_tiles(const F8Args &args, hipStream_t stream) {
+    typedef F8Core<WM, WN, FM, FN, GATED> C;
+    static thread_local int attr_device = -1;                // the attribute is per device (set again per thread: harmless)
+    int dev = -1;
+    if (hipError_t e = hipGetDevice(&dev)) return e;
+    if (attr_device != dev) {
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_f8_tiles<WM, WN, FM, FN, GATED>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS_BYTES)) return e;
+        attr_device = dev;
+    }
+    const int tiles_m = (args.m + C::BM - 1) / C::BM, tiles_n = (args.n + C::COLS - 1) / C::COLS;
+    const TileMap map = make_tile_map(tiles_m, tiles_n, tiles_m * tiles_n * args.ranges);
+    hipLaunchKernelGGL((k_f8_tiles<WM, WN, FM, FN, GATED>), dim3((unsigned)map.total), dim3(C::THREADS), C::LDS_BYTES, stream, args, map);
+    return hipGetLastError();
+}
+
+template <bool GATED>
+hipError_t launch_form(const F8Args &args, const F8Plan &plan, hipStream_t stream) {
+    if (hipError_t e = plan.form == F8Form::kLarge ? launch_tiles<4, 2, 4, 8, GATED>(args, stream) : launch_tiles<2, 2, 4, 4, GATED>(args, stream)) return e;
+    if (args.ranges == 1) return hipSuccess;
+    const int64_t threads = (int64_t)args.m * ((args.n + 3) / 4);
+    hipLaunchKernelGGL(k_f8_ranges<GATED>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, args);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_f8_product(const F8Args &args, const F8Plan &plan, bool gated, hipStream_t stream) {
+    if (plan.form == F8Form::kThin) return launch_f8_thin(args, gated, stream);
+    return gated ? launch_form<true>(args, plan, stream) : launch_form<false>(args, plan, stream);
+}
+
+}  // namespace oz2

@@ -54,6 +54,7 @@ struct F8Plan {
 };
 
 constexpr int kF8ThinRows = 64;
+constexpr int kF8WideBlocks = 3;           // what the kernel of large tiles needs of k, and one whole tile
 constexpr int kF8MaxRanges = 16;
 
 inline int64_t f8_blocks(int64_t k) { return (k + kF8Block - 1) / kF8Block; }
@@ -69,7 +70,7 @@ inline F8Plan f8_plan(int64_t m, int64_t n, int64_t k, bool gated) {
         return p;
     }
     const int64_t large = f8_tiles(m, wide, 256), small = f8_tiles(m, wide, 128);
-    if (large >= 192) {
+    if (large >= 192 && m >= 256 && wide >= 256 && blocks >= kF8WideBlocks) {
         p.form = F8Form::kLarge;
         return p;
     }
@@ -87,6 +88,7 @@ inline F8Plan f8_plan(int64_t m, int64_t n, int64_t k, bool gated) {
 
 #if defined(__HIPCC__)
 hipError_t launch_f8_product(const F8Args &args, const F8Plan &plan, bool gated, hipStream_t stream);
+hipError_t launch_f8_wide(const F8Args &args, bool gated, hipStream_t stream);
 hipError_t launch_f8_thin(const F8Args &args, bool gated, hipStream_t stream);
 
 // What a quantisation writes: either half may be missing (q == nullptr).

@@ -34,10 +34,12 @@ __device__ __forceinline__ f8_v4i f8_keep(f8_v4i v, int valid) {
 
 // Both activations are g / (1 + exp(-s)): s = g (SiLU), s = 2 sqrt(2 / pi) (g + 0.044715 g^3) (GELU, tanh form, since
 // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))).  Their slope is p + g p (1 - p) s' with p = 1 / (1 + exp(-s)).
-constexpr float kGeluScale = 1.5957691216057308f, kGeluCube = 0.044715f;
+// The exponential and the reciprocal are the hardware's, each within 1 or 2 units of the last place; with the rounding of s log2(e) the gate is within
+// (4 + |s|) 2^-24 of its value.
+constexpr float kGeluScale = 1.5957691216057308f, kGeluCube = 0.044715f, kMinusLog2E = -1.4426950408889634f;
 __device__ __forceinline__ float f8_gate(float g, int act) {
     const float s = act ? kGeluScale * __builtin_fmaf(kGeluCube * g * g, g, g) : g;
-    return 1.0f / (1.0f + expf(-s));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * kMinusLog2E));
 }
 __device__ __forceinline__ float f8_act(float g, int act) { return g * f8_gate(g, act); }
 __device__ __forceinline__ float f8_slope(float g, float p, int act) {
@@ -77,13 +79,14 @@ __device__ __forceinline__ void f8_store(void *C, int type, int64_t at, float x)
     else static_cast<float *>(C)[at] = x;
 }
 
-// N (a multiple of 4) numbers in a row from C[at] on, of which `valid` exist; vec: C + at is on a multiple of N bytes, at most 16.
+// N (a multiple of 4) numbers in a row at C[at], of which those from `from` to `valid` are written; vec: C + at is on a multiple of N numbers'
+// bytes, at most 16.
 template <int N>
-__device__ __forceinline__ void f8_store_row(void *C, int type, int64_t at, const float (&x)[N], int valid, bool vec) {
-    if (!vec || valid < N) {
+__device__ __forceinline__ void f8_store_row(void *C, int type, int64_t at, const float (&x)[N], int valid, bool vec, int from = 0) {
+    if (!vec || valid < N || from > 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (i < valid) f8_store(C, type, at + i, x[i]);
+            if (i >= from && i < valid) f8_store(C, type, at + i, x[i]);
         return;
     }
     if (type == kF8F32) {
@@ -111,13 +114,13 @@ __device__ __forceinline__ void f8_store_row(void *C, int type, int64_t at, cons
 
 // alpha * x + beta * C, and its store.
 template <int N>
-__device__ __forceinline__ void f8_update_row(const F8Out &o, int64_t at, float (&x)[N], int valid, bool vec) {
+__device__ __forceinline__ void f8_update_row(const F8Out &o, int64_t at, float (&x)[N], int valid, bool vec, int from = 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         x[i] *= o.alpha;
-        if (o.beta != 0.0f && i < valid) x[i] = __builtin_fmaf(o.beta, f8_load(o.C, o.type, at + i), x[i]);
+        if (o.beta != 0.0f && i >= from && i < valid) x[i] = __builtin_fmaf(o.beta, f8_load(o.C, o.type, at + i), x[i]);
     }
-    f8_store_row<N>(o.C, o.type, at, x, valid, vec);
+    f8_store_row<N>(o.C, o.type, at, x, valid, vec, from);
 }
 
 }  // namespace oz2

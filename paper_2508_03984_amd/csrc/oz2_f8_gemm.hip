@@ -239,7 +239,7 @@ hipError_t launch_tiles(const F8Args &args, hipStream_t stream) {
 
 template <bool GATED>
 hipError_t launch_form(const F8Args &args, const F8Plan &plan, hipStream_t stream) {
-    if (hipError_t e = plan.form == F8Form::kLarge ? launch_tiles<4, 2, 4, 8, GATED>(args, stream) : launch_tiles<2, 2, 4, 4, GATED>(args, stream)) return e;
+    if (hipError_t e = plan.form == F8Form::kLarge ? launch_f8_wide(args, GATED, stream) : launch_tiles<2, 2, 4, 4, GATED>(args, stream)) return e;
     if (args.ranges == 1) return hipSuccess;
     const int64_t threads = (int64_t)args.m * ((args.n + 3) / 4);
     hipLaunchKernelGGL(k_f8_ranges<GATED>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, args);

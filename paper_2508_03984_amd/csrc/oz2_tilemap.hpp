@@ -21,7 +21,8 @@ inline Divisor make_divisor(int d) {
     while (((int64_t)1 << s) < d) ++s;
     return Divisor{(uint32_t)(((uint64_t)1 << (31 + s)) / (uint64_t)d + 1), 31 + s};
 }
-OZ2_HOST_DEVICE inline int divide(int x, Divisor d) { return (int)((uint64_t)(uint32_t)x * d.mul >> d.shift); }
+OZ2_HOST_DEVICE inline int divide(int x, uint32_t mul, uint32_t shift) { return (int)((uint64_t)(uint32_t)x * mul >> shift); }
+OZ2_HOST_DEVICE inline int divide(int x, Divisor d) { return divide(x, d.mul, d.shift); }
 
 // Workgroup ids are handed to the 8 XCDs round-robin, and 256 workgroups run at a time (one per CU):
 // XCD x runs the ids = x (mod 8), 32 at a time.  Those 32 are given 32 consecutive positions of a walk over
@@ -65,33 +66,34 @@ inline TileMap make_tile_map(int tiles_m, int tiles_n, int total) {
     return t;
 }
 
-OZ2_HOST_DEVICE inline void map_tile(const TileMap &tm, int id, int &s, int &tr, int &tc) {
+// (MapPtr: a pointer to the map, of whatever address space it lies in)
+template <typename MapPtr>
+OZ2_HOST_DEVICE inline void map_tile_at(MapPtr tm, int id, int &s, int &tr, int &tc) {
     const int xcd = id & 7, local = id >> 3, round0 = id & ~255;
-    if (tm.regions_n) {
-        const int j = local & 31, region = id >> 8, regions = (tm.tiles_m >> 4) * tm.regions_n;
-        s = divide(region, tm.per_slice);
-        const int r = region - s * regions, r_row = divide(r, tm.row);
+    if (tm->regions_n) {
+        const int j = local & 31, region = id >> 8, regions = (tm->tiles_m >> 4) * tm->regions_n;
+        s = divide(region, tm->per_slice.mul, tm->per_slice.shift);
+        const int r = region - s * regions, r_row = divide(r, tm->row.mul, tm->row.shift);
         tr = r_row * 16 + (xcd >> 2) * 8 + (j >> 2);
-        tc = (r - r_row * tm.regions_n) * 16 + (xcd & 3) * 4 + (j & 3);
+        tc = (r - r_row * tm->regions_n) * 16 + (xcd & 3) * 4 + (j & 3);
         return;
     }
-    const int left = tm.total - round0;                    // tiles from this round on; a last round is dealt evenly
+    const int left = tm->total - round0;                    // tiles from this round on; a last round is dealt evenly
     const int each = left < 256 ? left >> 3 : 32, more = left < 256 ? left & 7 : 0;
     const int pos = round0 + xcd * each + (xcd < more ? xcd : more) + (local & 31);
-    s = divide(pos, tm.per_slice);
-    int w = pos - s * (tm.tiles_m * tm.tiles_n);
+    s = divide(pos, tm->per_slice.mul, tm->per_slice.shift);
+    int w = pos - s * (tm->tiles_m * tm->tiles_n);
     // the pair of bands: its rows take the positions [first row, last row] * tiles_n
-    const int wide_rows = tm.wide_bands * (tm.band_rows + 1), v = divide(w, tm.row);
-    const int band = (v < wide_rows ? divide(v, tm.wide) : tm.wide_bands + divide(v - wide_rows, tm.narrow)) & ~1;
-    const int row0 = band * tm.band_rows + (band < tm.wide_bands ? band : tm.wide_bands);
-    const int upper = tm.band_rows + (band < tm.wide_bands ? 1 : 0);
-    const int lower = band + 1 < tm.bands ? tm.band_rows + (band + 1 < tm.wide_bands ? 1 : 0) : 0;
-    w -= row0 * tm.tiles_n;
+    const int wide_rows = tm->wide_bands * (tm->band_rows + 1), v = divide(w, tm->row.mul, tm->row.shift);
+    const int band = (v < wide_rows ? divide(v, tm->wide.mul, tm->wide.shift) : tm->wide_bands + divide(v - wide_rows, tm->narrow.mul, tm->narrow.shift)) & ~1;
+    const int row0 = band * tm->band_rows + (band < tm->wide_bands ? band : tm->wide_bands);
+    const int upper = tm->band_rows + (band < tm->wide_bands ? 1 : 0);
+    const int lower = band + 1 < tm->bands ? tm->band_rows + (band + 1 < tm->wide_bands ? 1 : 0) : 0;
+    w -= row0 * tm->tiles_n;
     // (the last band is never a wide one)
-    const Divisor by_group = band + 1 >= tm.bands ? tm.group[3] : band + 1 < tm.wide_bands ? tm.group[0]
-                                                  : band < tm.wide_bands ? tm.group[1] : tm.group[2];
-    const int group = divide(w, by_group), col0 = 4 * group;
-    const int cols = tm.tiles_n - col0 < 4 ? tm.tiles_n - col0 : 4;
+    const int which = band + 1 >= tm->bands ? 3 : band + 1 < tm->wide_bands ? 0 : band < tm->wide_bands ? 1 : 2;
+    const int group = divide(w, tm->group[which].mul, tm->group[which].shift), col0 = 4 * group;
+    const int cols = tm->tiles_n - col0 < 4 ? tm->tiles_n - col0 : 4;
     w -= group * 4 * (upper + lower);
     const bool low = w >= upper * cols;
     if (low) w -= upper * cols;
@@ -99,6 +101,7 @@ OZ2_HOST_DEVICE inline void map_tile(const TileMap &tm, int id, int &s, int &tr,
     tr = row0 + (low ? upper : 0) + row;
     tc = col0 + w - row * cols;
 }
+OZ2_HOST_DEVICE inline void map_tile(const TileMap &tm, int id, int &s, int &tr, int &tc) { map_tile_at(&tm, id, s, tr, tc); }
 
 // The work of a launch with one workgroup per tile: the tiles of all slices, each slice once per K range (a `slice` of the map is
 // (range, slice), the slices of a range together).  Tiles of 128 x 128 that hold nothing but padding are not among them: they are

@@ -37,14 +37,37 @@ __device__ __forceinline__ f8_v4i f8_keep(f8_v4i v, int valid) {
 // The exponential and the reciprocal are the hardware's, each within 1 or 2 units of the last place; with the rounding of s log2(e) the gate is within
 // (4 + |s|) 2^-24 of its value.
 constexpr float kGeluScale = 1.5957691216057308f, kGeluCube = 0.044715f, kMinusLog2E = -1.4426950408889634f;
-__device__ __forceinline__ float f8_gate(float g, int act) {
-    const float s = act ? kGeluScale * __builtin_fmaf(kGeluCube * g * g, g, g) : g;
+template <int ACT>
+__device__ __forceinline__ float f8_gate(float g) {
+    const float s = ACT ? kGeluScale * __builtin_fmaf(kGeluCube * g * g, g, g) : g;
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * kMinusLog2E));
 }
-__device__ __forceinline__ float f8_act(float g, int act) { return g * f8_gate(g, act); }
-__device__ __forceinline__ float f8_slope(float g, float p, int act) {
-    const float ds = act ? kGeluScale * __builtin_fmaf(3.0f * kGeluCube * g, g, 1.0f) : 1.0f, q = p * (1.0f - p);
+template <int ACT>
+__device__ __forceinline__ float f8_slope(float g, float p) {
+    const float ds = ACT ? kGeluScale * __builtin_fmaf(3.0f * kGeluCube * g, g, 1.0f) : 1.0f, q = p * (1.0f - p);
+    if (!ACT) return __builtin_fmaf(g, q, p);
     return q > 0.0f ? __builtin_fmaf(g * q, ds, p) : p;         // p is 0 or 1 (or NaN): the slope's limit, also where s' overflows
+}
+// x <- act(x) u for several numbers, with one branch for all of them; the two gradients, h act(g) and h u act'(g).
+template <int N>
+__device__ __forceinline__ void f8_gated(float (&x)[N], const float (&u)[N], int act) {
+    if (act) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = x[e] * f8_gate<1>(x[e]) * u[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = x[e] * f8_gate<0>(x[e]) * u[e];
+    }
+}
+template <int ACT, int N>
+__device__ __forceinline__ void f8_times_act(const float (&g)[N], const float (&h)[N], float (&x)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = h[e] * (g[e] * f8_gate<ACT>(g[e]));
+}
+template <int ACT, int N>
+__device__ __forceinline__ void f8_times_slope(const float (&g)[N], const float (&u)[N], const float (&h)[N], float (&x)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = h[e] * u[e] * f8_slope<ACT>(g[e], f8_gate<ACT>(g[e]));
 }
 
 // Numbers of one type from and to binary32, rounded to nearest even.

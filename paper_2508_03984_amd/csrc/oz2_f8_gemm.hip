@@ -185,8 +185,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_f8_tiles(F8Args p, TileMap m
                     f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + col, x, valid, o.z_vec);
                     f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + p.up + col, u, valid, o.z_vec);
                 }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = f8_act(x[e], o.act) * u[e];
+                f8_gated(x, u, o.act);
                 f8_store_row<16>(o.C, o.type, (int64_t)row * o.ldc + col, x, valid, o.vec);
             }
         }
@@ -214,8 +213,7 @@ __global__ __launch_bounds__(256) void k_f8_ranges(F8Args p) {
             f8_store_row<4>(o.Z, o.type, row * o.ldz + col, x, valid, o.z_vec);
             f8_store_row<4>(o.Z, o.type, row * o.ldz + p.up + col, u, valid, o.z_vec);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = f8_act(x[e], o.act) * u[e];
+        f8_gated(x, u, o.act);
         f8_store_row<4>(o.C, o.type, row * o.ldc + col, x, valid, o.vec);
     }
 }

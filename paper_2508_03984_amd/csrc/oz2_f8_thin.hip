@@ -109,8 +109,7 @@ __global__ __launch_bounds__(512) void k_f8_thin(F8Args p) {
                 f8_store_row<4>(o.Z, o.type, row * o.ldz + col, x, valid, o.z_vec);
                 f8_store_row<4>(o.Z, o.type, row * o.ldz + p.up + col, u, valid, o.z_vec);
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = f8_act(x[e], o.act) * u[e];
+            f8_gated(x, u, o.act);
             f8_store_row<4>(o.C, o.type, row * o.ldc + col, x, valid, o.vec);
         }
     }

@@ -369,8 +369,7 @@ struct Wide {
                     store_16_bits<TYPE>(z + i * 16 * o.ldz, x);
                     store_16_bits<TYPE>(z + i * 16 * o.ldz + up, y);
                 }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = f8_act(x[e], o.act) * y[e];
+                f8_gated(x, y, o.act);
                 store_16_bits<TYPE>(c + i * 16 * o.ldc, x);
             } else {
 #pragma unroll
@@ -427,8 +426,7 @@ struct Wide {
                     f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + col, x, 16, z_vec, from);
                     f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + up + col, u, 16, z_vec, from);
                 }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = f8_act(x[e], o.act) * u[e];
+                f8_gated(x, u, o.act);
                 f8_store_row<16>(o.C, o.type, (int64_t)row * o.ldc + col, x, 16, vec, from);
             }
         }

@@ -608,7 +608,7 @@ class F8:
     two of its blocks (torch.float8_e8m0fnu), of `block_rows` (1 or 128) x 128 elements.  Keep it as long as the tensors' memory: a call reads
     the addresses from here."""
 
-    __slots__ = ("q", "scale", "block_rows", "ref", "_struct")
+    __slots__ = ("q", "scale", "block_rows", "rows", "cols", "ref", "_struct")
 
     def __init__(self, q, scale, block_rows: int):
         torch = _th()
@@ -625,7 +625,7 @@ class F8:
             left = t.untyped_storage().nbytes() - t.storage_offset() - (t.shape[0] - 1) * t.stride(0)
             if t.numel() and left < _up(row, unit):
                 raise ValueError(f"rows have to be stored up to the next multiple of {unit} bytes")
-        self.q, self.scale, self.block_rows = q, scale, block_rows
+        self.q, self.scale, self.block_rows, self.rows, self.cols = q, scale, block_rows, rows, cols
         self._struct = _F8Struct(_dev(q), ld, _dev(scale), ld_scale, block_rows)
         self.ref = C.byref(self._struct)
 
@@ -651,25 +651,26 @@ class F8:
         return tuple(self.q.shape)
 
 
-_f8_types = None
+_f8_types = {}
 
 
 def _f8_type(t) -> int:
-    global _f8_types
-    if _f8_types is None:
+    got = _f8_types.get(t.dtype)
+    if got is None:
         torch = _th()
-        _f8_types = {torch.bfloat16: OZ2_BF16, torch.float16: OZ2_F16, torch.float32: OZ2_F32}
-    if t.dtype not in _f8_types:
-        raise ValueError(f"tensor of dtype bfloat16, float16 or float32 expected, got {t.dtype}")
-    return _f8_types[t.dtype]
+        _f8_types.update({torch.bfloat16: OZ2_BF16, torch.float16: OZ2_F16, torch.float32: OZ2_F32})
+        if t.dtype not in _f8_types:
+            raise ValueError(f"tensor of dtype bfloat16, float16 or float32 expected, got {t.dtype}")
+        got = _f8_types[t.dtype]
+    return got
 
 
 def _f8_ref(x, rows: int, cols: int):
     """The struct of a matrix that has at least rows x cols elements; None for None."""
     if x is None:
         return None
-    if x.q.shape[0] < rows or x.q.shape[1] < cols:
-        raise ValueError(f"matrix of {rows} x {cols} elements in 8 bits expected, got {x.q.shape[0]} x {x.q.shape[1]}")
+    if x.rows < rows or x.cols < cols:
+        raise ValueError(f"matrix of {rows} x {cols} elements in 8 bits expected, got {x.rows} x {x.cols}")
     return x.ref
 
 

@@ -948,7 +948,6 @@ bool f8_type_ok(int type) { return type == kF8Bf16 || type == kF8F16 || type == 
 bool f8_numbers_ok(const void *p, int64_t ld, int64_t cols, int type) {
     return p && ld >= cols && reinterpret_cast<uintptr_t>(p) % f8_type_bytes(type) == 0;
 }
-int f8_vec(const void *p, int64_t ld, int type) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * f8_type_bytes(type) % 16 == 0; }
 
 // m, n (columns of C), k of a product; kNothing: there is nothing to do.
 oz2_status f8_sizes(int64_t m, int64_t n, int64_t k, int type, bool *nothing) {
@@ -968,10 +967,7 @@ oz2_status f8_run(Ctx &g, F8Args &args, bool gated, hipStream_t stream) {
             args.out.planes = reinterpret_cast<float *>(g.ws);
             args.out.ldp = f8_plane_ld(args.n, gated);
             args.out.plane = (int64_t)args.m * args.out.ldp;
-        } else {
-            plan.ranges = 1;
-            plan.kb_each = (int)f8_blocks(args.k);
-        }
+        } else plan = f8_plan_one_range(args.m, args.n, args.k, gated);
     }
     args.ranges = plan.ranges;
     args.kb_each = plan.kb_each;
@@ -1010,7 +1006,7 @@ oz2_status oz2_ctx_f8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, fl
         if (oz2_status st = f8_matrix(B, k, &args.B)) return st;
     }
     args.m = (int)m; args.n = (int)n; args.k = (int)k;
-    args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.vec = f8_vec(C, ldc, type);
+    args.out.C = C; args.out.ldc = ldc; args.out.type = type;
     args.out.alpha = alpha; args.out.beta = beta;
     return f8_run(resolve(ctx), args, false, stream);
 }
@@ -1034,9 +1030,9 @@ oz2_status oz2_ctx_f8_gated(oz2_context *ctx, int64_t m, int64_t f, int64_t k, o
         if (oz2_status st = f8_matrix(W, k, &args.B)) return st;
     }
     args.m = (int)m; args.n = (int)f; args.k = (int)k; args.up = (int)up;
-    args.out.C = H; args.out.ldc = ldh; args.out.type = type; args.out.vec = f8_vec(H, ldh, type);
+    args.out.C = H; args.out.ldc = ldh; args.out.type = type;
     args.out.alpha = 1.0f; args.out.act = act;
-    args.out.Z = Z; args.out.ldz = ldz; args.out.z_vec = Z && f8_vec(Z, ldz, type);
+    args.out.Z = Z; args.out.ldz = ldz;
     return f8_run(resolve(ctx), args, true, stream);
 }
 

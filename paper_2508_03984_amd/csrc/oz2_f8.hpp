@@ -27,12 +27,10 @@ struct F8Out {
     void *C;
     int64_t ldc;
     int type;
-    int vec;                               // rows of C allow 16-byte accesses at columns that are multiples of 16
     float alpha, beta;
     int act;
     void *Z;                               // nullptr: not wanted
     int64_t ldz;
-    int z_vec;
     float *planes;                         // sums of K ranges: [range][m][ldp]; gated: the up part from column ldp / 2 on
     int64_t plane, ldp;
 };
@@ -46,11 +44,14 @@ struct F8Args {
 };
 
 // ------------------------------------------------------------------ which kernel
-enum class F8Form { kThin, kSmall, kLarge };
+// kThin: few rows of A, B read once into registers (oz2_f8_thin.hip); the others tiles of 64, 128 (oz2_f8_gemm.hip) or 256 rows and
+// columns (oz2_f8_wide.hip), which may cut k into ranges whose sums are added by a second kernel.
+enum class F8Form { kThin, kSmall, kMiddle, kLarge };
 struct F8Plan {
     F8Form form;
-    int ranges, kb_each;
+    int ranges, kb_each;                   // K ranges, and blocks of each (a multiple of 4 if there are several)
     size_t plane_bytes;                    // workspace for the planes of the ranges (0: none needed)
+    double us;                             // what it is expected to take
 };
 
 constexpr int kF8ThinRows = 64;
@@ -58,31 +59,66 @@ constexpr int kF8WideBlocks = 3;           // what the kernel of large tiles nee
 constexpr int kF8MaxRanges = 16;
 
 inline int64_t f8_blocks(int64_t k) { return (k + kF8Block - 1) / kF8Block; }
-inline int64_t f8_tiles(int64_t rows, int64_t cols, int tile) { return ((rows + tile - 1) / tile) * ((cols + tile - 1) / tile); }
+inline int64_t f8_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t f8_tiles(int64_t rows, int64_t cols, int tile) { return f8_ceil(rows, tile) * f8_ceil(cols, tile); }
 // Columns of a plane: those of C, or of both sums; rows of a plane start at multiples of 64 bytes.
-inline int64_t f8_plane_ld(int64_t n, bool gated) { return (n + 15) / 16 * 16 * (gated ? 2 : 1); }
+inline int64_t f8_plane_ld(int64_t n, bool gated) { return f8_ceil(n, 16) * 16 * (gated ? 2 : 1); }
+
+// Of tiles of one size, what a call takes: so many microseconds once, and for each round of the compute units a time per tile and per block of k
+// (and, of both together, more where two small tiles share a unit).  Fitted to calls of 20 shapes from 65 x 8192 x 8192 to
+// 4096^3 in a graph, each with tiles of all sizes and with 1 to 16 ranges; off by 10 % mostly, 30 % at most.  Some, in us, tiles of 64 | 128 |
+// 256: 500 x 300 x 777 6.4 | 13.4 | 35; 512 x 4096 x 4096 18.8 | 27 | 38; 1024 x 4096 x 4096 33 | 28.8 | 46; 2048^3 20.6 | 17.6 | 28;
+// 3000^3 58 | 64 | 49; 4096 x 4096 x 512 31 | 30 | 19; 4096^3 121 | 102 | 62; with ranges: 65 x 8192 x 8192 24.2 -> 22.2 (2 ranges, tiles of
+// 64), 2048 x 2048 x 16384 90 (one, 128) -> 85 (4, 256), 1536 x 1000 x 40000 117 (2, 128) -> 84 (10, 256).
+struct F8Cost {
+    int tile, slots;
+    double once, per_tile, per_block;
+};
+constexpr F8Cost kF8Costs[3] = {{64, 512, 3.5, 1.8, 0.40}, {128, 256, 4.0, 4.0, 0.64}, {256, 256, 13.0, 0.0, 1.55}};
+constexpr double kF8AlonePerBlock = 0.285;                     // a tile of 64 with a unit of its own
+constexpr double kF8RangesOnce = 3.0, kF8PlaneBytesPerUs = 3.2e6;   // the second kernel; planes are written and read
+constexpr double kF8BytesPerUs = 5.2e6;                        // from HBM
+
+// The form for few rows: one group of 4 blocks per wavefront at a time, B from HBM, A from the caches for every 16 columns.  In us, this form |
+// the best of the others: 1 x 8192 x 8192 13.7 | 16.2; 17 x 4096 x 4096 7.3 | 10.1; 33 x 2048 x 2048 5.9 | 7.3; 17 x 8192 x 8192 20.5 | 16.6;
+// 64 x 8192 x 8192 41.6 | 18.1.
+inline double f8_thin_us(int64_t m, int64_t n, int64_t k, bool gated) {
+    const double wide = gated ? 2.0 * n : n, steps = f8_ceil(f8_blocks(k), 4 * 8);
+    return std::max(1.0 + 2.5 * steps, 1.0 + wide * k / kF8BytesPerUs) + f8_ceil(n, 16) * (double)m * k / 9.4e6;
+}
 
 inline F8Plan f8_plan(int64_t m, int64_t n, int64_t k, bool gated) {
-    const int64_t wide = gated ? 2 * n : n, blocks = f8_blocks(k);
-    F8Plan p{F8Form::kSmall, 1, (int)std::max<int64_t>(blocks, 1), 0};
+    const int64_t wide = gated ? 2 * n : n, blocks = f8_blocks(k), groups = f8_ceil(blocks, 4);
+    F8Plan best{F8Form::kMiddle, 1, (int)std::max<int64_t>(blocks, 1), 0, 1e30};
     if (m <= kF8ThinRows) {
-        p.form = F8Form::kThin;
-        return p;
+        best.form = F8Form::kThin;
+        best.us = f8_thin_us(m, n, k, gated);
     }
-    const int64_t large = f8_tiles(m, wide, 256), small = f8_tiles(m, wide, 128);
-    if (large >= 192 && m >= 256 && wide >= 256 && blocks >= kF8WideBlocks) {
-        p.form = F8Form::kLarge;
-        return p;
+    for (int f = 0; f < 3; ++f) {
+        const F8Cost &c = kF8Costs[f];
+        if (c.tile == 256 && (m < 256 || wide < 256)) continue;
+        const int64_t tiles = f8_ceil(m, c.tile) * f8_ceil(n, gated ? c.tile / 2 : c.tile);
+        int64_t last = 0;
+        for (int64_t asked = 1; asked <= std::min<int64_t>(std::max<int64_t>(groups, 1), kF8MaxRanges); ++asked) {
+            const int64_t each = asked == 1 ? std::max<int64_t>(blocks, 1) : f8_ceil(groups, asked) * 4, ranges = std::max<int64_t>(f8_ceil(blocks, each), 1);
+            if (ranges == last) continue;
+            last = ranges;
+            if (c.tile == 256 && blocks - (ranges - 1) * each < kF8WideBlocks) continue;
+            const int64_t items = tiles * ranges, rounds = f8_ceil(items, c.slots);
+            const double per_block = f == 0 && items <= 256 ? kF8AlonePerBlock : c.per_block;
+            const size_t planes = ranges == 1 ? 0 : (size_t)ranges * (size_t)m * (size_t)f8_plane_ld(n, gated) * 4;
+            const double us = std::max(c.once + rounds * (c.per_tile + each * per_block), 3.0 + (double)(m + wide) * k / kF8BytesPerUs) + (planes ? kF8RangesOnce + planes / kF8PlaneBytesPerUs : 0.0);
+            if (us < best.us) best = F8Plan{(F8Form)(f + 1), (int)ranges, (int)each, planes, us};
+        }
     }
-    const int64_t groups = (blocks + 3) / 4;               // ranges are whole groups of 4 blocks
-    int64_t ranges = std::min<int64_t>({512 / std::max<int64_t>(small, 1), groups / 2, kF8MaxRanges});
-    if (ranges > 1) {
-        const int64_t each = (groups + ranges - 1) / ranges;
-        ranges = (groups + each - 1) / each;               // none empty
-        p.ranges = (int)ranges;
-        p.kb_each = (int)each * 4;
-        p.plane_bytes = (size_t)ranges * (size_t)m * (size_t)f8_plane_ld(n, gated) * 4;
-    }
+    return best;
+}
+// The same without planes.
+inline F8Plan f8_plan_one_range(int64_t m, int64_t n, int64_t k, bool gated) {
+    F8Plan p = f8_plan(m, n, k, gated);
+    p.ranges = 1;
+    p.kb_each = (int)std::max<int64_t>(f8_blocks(k), 1);
+    p.plane_bytes = 0;
     return p;
 }
 

@@ -102,19 +102,23 @@ __device__ __forceinline__ void f8_store(void *C, int type, int64_t at, float x)
     else static_cast<float *>(C)[at] = x;
 }
 
-// N (a multiple of 4) numbers in a row at C[at], of which those from `from` to `valid` are written; vec: C + at is on a multiple of N numbers'
-// bytes, at most 16.
+// N (a multiple of 4) numbers in a row at C[at], of which those from `from` to `valid` are written.  Whole rows go 16 bytes at a time, on
+// whatever multiple of the type's size they lie.
 template <int N>
-__device__ __forceinline__ void f8_store_row(void *C, int type, int64_t at, const float (&x)[N], int valid, bool vec, int from = 0) {
-    if (!vec || valid < N || from > 0) {
+__device__ __forceinline__ void f8_store_row(void *C, int type, int64_t at, const float (&x)[N], int valid, int from = 0) {
+    if (valid < N || from > 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i >= from && i < valid) f8_store(C, type, at + i, x[i]);
         return;
     }
     if (type == kF8F32) {
+        float *const to = static_cast<float *>(C) + at;
 #pragma unroll
-        for (int i = 0; i < N; i += 4) *reinterpret_cast<f8_v4f *>(static_cast<float *>(C) + at + i) = f8_v4f{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        for (int i = 0; i < N; i += 4) {
+            const f8_v4f w{x[i], x[i + 1], x[i + 2], x[i + 3]};
+            __builtin_memcpy(to + i, &w, 16);
+        }
         return;
     }
     uint32_t w[N / 2];
@@ -127,23 +131,25 @@ __device__ __forceinline__ void f8_store_row(void *C, int type, int64_t at, cons
     }
     uint16_t *const to = static_cast<uint16_t *>(C) + at;
     if constexpr (N == 4) {
-        *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+        __builtin_memcpy(to, w, 8);
     } else {
 #pragma unroll
-        for (int i = 0; i < N / 8; ++i)
-            reinterpret_cast<f8_v4i *>(to)[i] = f8_v4i{(int)w[4 * i], (int)w[4 * i + 1], (int)w[4 * i + 2], (int)w[4 * i + 3]};
+        for (int i = 0; i < N / 8; ++i) {
+            const f8_v4i v{(int)w[4 * i], (int)w[4 * i + 1], (int)w[4 * i + 2], (int)w[4 * i + 3]};
+            __builtin_memcpy(to + 8 * i, &v, 16);
+        }
     }
 }
 
 // alpha * x + beta * C, and its store.
 template <int N>
-__device__ __forceinline__ void f8_update_row(const F8Out &o, int64_t at, float (&x)[N], int valid, bool vec, int from = 0) {
+__device__ __forceinline__ void f8_update_row(const F8Out &o, int64_t at, float (&x)[N], int valid, int from = 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         x[i] *= o.alpha;
         if (o.beta != 0.0f && i >= from && i < valid) x[i] = __builtin_fmaf(o.beta, f8_load(o.C, o.type, at + i), x[i]);
     }
-    f8_store_row<N>(o.C, o.type, at, x, valid, vec, from);
+    f8_store_row<N>(o.C, o.type, at, x, valid, from);
 }
 
 }  // namespace oz2

@@ -8,9 +8,11 @@
 namespace oz2 {
 namespace {
 
+constexpr int kWaves = 8;                                     // of a workgroup at most (with 16, 1 x 16 x 16384 takes as long: its unit's loads bound it)
+
 // MT blocks of 16 rows of A.
 template <int MT, bool GATED>
-__global__ __launch_bounds__(512) void k_f8_thin(F8Args p) {
+__global__ __launch_bounds__(kWaves * 64) void k_f8_thin(F8Args p) {
     constexpr int SIDES = GATED ? 2 : 1;
     extern __shared__ f8_v4f sums[];                          // [wavefronts][SIDES * MT][64]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (int)blockDim.x >> 6;
@@ -43,6 +45,12 @@ __global__ __launch_bounds__(512) void k_f8_thin(F8Args p) {
         for (int s = 0; s < SIDES; ++s) sb[s] = *reinterpret_cast<const int *>(b_scale[s] + kb);
 #pragma unroll
         for (int t = 0; t < MT; ++t) sa[t] = *reinterpret_cast<const int *>(a_scale[t] + kb);
+        const auto multiply = [&](const f8_v8i(&x)[SIDES], const f8_v8i(&y)[MT], int u) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int s = 0; s < SIDES; ++s) acc[s][t] = f8_mfma(x[s], y[t], acc[s][t], (int)((uint32_t)sb[s] >> 8 * u), (int)((uint32_t)sa[t] >> 8 * u));
+        };
         if (kb + 4 <= whole) {
             f8_v8i x[4][SIDES], y[4][MT];
 #pragma unroll
@@ -56,32 +64,33 @@ __global__ __launch_bounds__(512) void k_f8_thin(F8Args p) {
                     y[u][t] = f8_join(*reinterpret_cast<const f8_v4i *>(a[t] + at), *reinterpret_cast<const f8_v4i *>(a[t] + at + 64));
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int s = 0; s < SIDES; ++s)
-                        acc[s][t] = f8_mfma(x[u][s], y[u][t], acc[s][t], (int)((uint32_t)sb[s] >> 8 * u), (int)((uint32_t)sa[t] >> 8 * u));
+            for (int u = 0; u < 4; ++u) multiply(x[u], y[u], u);
             continue;
         }
-        // The blocks at the end of k: chunks of 16 bytes are read if they begin before k, and cut there.
-        for (int u = 0; u < 4 && kb + u < KB; ++u) {
-            const int64_t at = (int64_t)(kb + u) * kF8Block;
-            const int left = p.k - (kb + u) * kF8Block - quarter * 16;    // of k from this lane's first chunk on
-            const auto read = [&](const uint8_t *row) {
-                const f8_v4i none{0, 0, 0, 0};
-                const f8_v4i lo = left > 0 ? f8_keep(*reinterpret_cast<const f8_v4i *>(row + at), left) : none;
-                const f8_v4i hi = left > 64 ? f8_keep(*reinterpret_cast<const f8_v4i *>(row + at + 64), left - 64) : none;
-                return f8_join(lo, hi);
-            };
-            f8_v8i x[SIDES];
+        // The blocks at the end of k, two at a time: chunks of 16 bytes that begin behind k are read as the row's last one, and all are cut at k.
+        const int last = (p.k - 1) / 16 * 16 - quarter * 16;
+        for (int u0 = 0; u0 < 4 && kb + u0 < KB; u0 += 2) {
+            f8_v4i x[2][SIDES][2], y[2][MT][2];
 #pragma unroll
-            for (int s = 0; s < SIDES; ++s) x[s] = read(b[s]);
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                const f8_v8i y = read(a[t]);
+                for (int half = 0; half < 2; ++half) {
+                    const int64_t at = min((kb + u0 + u) * kF8Block + half * 64, last);
 #pragma unroll
-                for (int s = 0; s < SIDES; ++s) acc[s][t] = f8_mfma(x[s], y, acc[s][t], (int)((uint32_t)sb[s] >> 8 * u), (int)((uint32_t)sa[t] >> 8 * u));
+                    for (int s = 0; s < SIDES; ++s) x[u][s][half] = *reinterpret_cast<const f8_v4i *>(b[s] + at);
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) y[u][t][half] = *reinterpret_cast<const f8_v4i *>(a[t] + at);
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (kb + u0 + u >= KB) break;                 // uniform (the scales behind k may be anything, NaN too)
+                const int left = p.k - (kb + u0 + u) * kF8Block - quarter * 16;
+                f8_v8i xs[SIDES], ys[MT];
+#pragma unroll
+                for (int s = 0; s < SIDES; ++s) xs[s] = f8_join(f8_keep(x[u][s][0], left), f8_keep(x[u][s][1], left - 64));
+#pragma unroll
+                for (int t = 0; t < MT; ++t) ys[t] = f8_join(f8_keep(y[u][t][0], left), f8_keep(y[u][t][1], left - 64));
+                multiply(xs, ys, u0 + u);
             }
         }
     }
@@ -102,15 +111,15 @@ __global__ __launch_bounds__(512) void k_f8_thin(F8Args p) {
         }
         if (row >= p.m || valid <= 0) continue;
         float x[4] = {s[0], s[1], s[2], s[3]};
-        if constexpr (!GATED) f8_update_row<4>(o, row * o.ldc + col, x, valid, o.vec);
+        if constexpr (!GATED) f8_update_row<4>(o, row * o.ldc + col, x, valid);
         else {
             float u[4] = {v[0], v[1], v[2], v[3]};
             if (o.Z) {
-                f8_store_row<4>(o.Z, o.type, row * o.ldz + col, x, valid, o.z_vec);
-                f8_store_row<4>(o.Z, o.type, row * o.ldz + p.up + col, u, valid, o.z_vec);
+                f8_store_row<4>(o.Z, o.type, row * o.ldz + col, x, valid);
+                f8_store_row<4>(o.Z, o.type, row * o.ldz + p.up + col, u, valid);
             }
             f8_gated(x, u, o.act);
-            f8_store_row<4>(o.C, o.type, row * o.ldc + col, x, valid, o.vec);
+            f8_store_row<4>(o.C, o.type, row * o.ldc + col, x, valid);
         }
     }
 }
@@ -118,7 +127,7 @@ __global__ __launch_bounds__(512) void k_f8_thin(F8Args p) {
 template <int MT, bool GATED>
 hipError_t launch(const F8Args &args, hipStream_t stream) {
     const int groups = (args.k + 4 * kF8Block - 1) / (4 * kF8Block);
-    const int waves = groups <= 1 ? 1 : groups <= 2 ? 2 : groups <= 4 ? 4 : 8;
+    const int waves = groups <= 1 ? 1 : groups <= 2 ? 2 : groups <= 4 ? 4 : kWaves;
     const size_t lds_bytes = (size_t)waves * MT * (GATED ? 2 : 1) * 1024;
     hipLaunchKernelGGL((k_f8_thin<MT, GATED>), dim3((unsigned)((args.n + 15) / 16)), dim3(waves * 64), lds_bytes, stream, args);
     return hipGetLastError();

@@ -350,8 +350,8 @@ struct Wide {
             hi[b] = F8Number<TYPE>::pack(x[4 * b + 2], x[4 * b + 3]);
         }
         const exchanged_t l = exchange_quarters(lo), h = exchange_quarters(hi);
-        reinterpret_cast<f8_v4i *>(to)[0] = f8_v4i{l[0], h[0], l[1], h[1]};
-        reinterpret_cast<f8_v4i *>(to)[1] = f8_v4i{l[2], h[2], l[3], h[3]};
+        const f8_v4i w[2] = {{l[0], h[0], l[1], h[1]}, {l[2], h[2], l[3], h[3]}};
+        __builtin_memcpy(to, w, 32);                           // (wherever C lies)
     }
     // The results of a whole tile in 16 bits.
     template <int TYPE>
@@ -381,18 +381,20 @@ struct Wide {
         });
     }
     // The results of any tile, 16 rows at a time; this code exists once.
-    __device__ __forceinline__ void store(const Item &it) const {
+    __device__ __forceinline__ void store(const Item &it, void *c, void *z, float *planes) const {
         const ArgsPtr a = arguments();
-        const F8Out o = fetch(&a->p.out);
+        F8Out o = fetch(&a->p.out);
+        o.C = c;                                               // (known to be in global memory, unlike what is fetched)
+        o.Z = z;
+        o.planes = planes;
         const int m = a->p.m, n = a->p.n, up = a->p.up;
         const int row0 = min(it.tr * 256, m - 256), col0 = min(it.tc * COLS, n - COLS);
-        if (row0 == it.tr * 256 && col0 == it.tc * COLS && o.type != kF8F32 && o.vec && o.beta == 0.0f && !o.planes && (!GATED || !o.Z || o.z_vec)) {
+        if (row0 == it.tr * 256 && col0 == it.tc * COLS && o.type != kF8F32 && o.beta == 0.0f && !o.planes) {
             if (o.type == kF8Bf16) store_whole<kF8Bf16>(it, o, up);
             else store_whole<kF8F16>(it, o, up);
             return;
         }
         const int first = row0 + (wave >> 1) * 128 + lrow;
-        const bool vec = o.vec && (col0 & 15) == 0, z_vec = o.z_vec && (col0 & 15) == 0;
 #pragma unroll 1
         for (int unit = 0; unit < 16; ++unit) {
             float x[16], u[16];
@@ -411,30 +413,30 @@ struct Wide {
             exchange(x);
             if constexpr (!GATED) {
                 if (!ours) continue;
-                if (o.planes) f8_store_row<16>(o.planes, kF8F32, it.range * o.plane + (int64_t)row * o.ldp + col, x, 16, (col0 & 15) == 0, from);
-                else f8_update_row<16>(o, (int64_t)row * o.ldc + col, x, 16, vec, from);
+                if (o.planes) f8_store_row<16>(o.planes, kF8F32, it.range * o.plane + (int64_t)row * o.ldp + col, x, 16, from);
+                else f8_update_row<16>(o, (int64_t)row * o.ldc + col, x, 16, from);
             } else {
                 exchange(u);
                 if (!ours) continue;
                 if (o.planes) {
                     const int64_t at = it.range * o.plane + (int64_t)row * o.ldp + col;
-                    f8_store_row<16>(o.planes, kF8F32, at, x, 16, (col0 & 15) == 0, from);
-                    f8_store_row<16>(o.planes, kF8F32, at + o.ldp / 2, u, 16, (col0 & 15) == 0, from);
+                    f8_store_row<16>(o.planes, kF8F32, at, x, 16, from);
+                    f8_store_row<16>(o.planes, kF8F32, at + o.ldp / 2, u, 16, from);
                     continue;
                 }
                 if (o.Z) {
-                    f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + col, x, 16, z_vec, from);
-                    f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + up + col, u, 16, z_vec, from);
+                    f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + col, x, 16, from);
+                    f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + up + col, u, 16, from);
                 }
                 f8_gated(x, u, o.act);
-                f8_store_row<16>(o.C, o.type, (int64_t)row * o.ldc + col, x, 16, vec, from);
+                f8_store_row<16>(o.C, o.type, (int64_t)row * o.ldc + col, x, 16, from);
             }
         }
     }
 };
 
 template <bool GATED>
-__global__ __launch_bounds__(256, 1) void k_f8_wide(WideArgs) {
+__global__ __launch_bounds__(256, 1) void k_f8_wide(WideArgs args) {
     typedef Wide<GATED> W;
     claim_accumulators();
     W w;
@@ -490,7 +492,7 @@ __global__ __launch_bounds__(256, 1) void k_f8_wide(WideArgs) {
         if (((kb1 - kb0) & 3) != 0) scales ^= 1;                      // (a fourth block has changed it)
         // The accumulators are complete, and so are this wavefront's loads of the next tile's first two blocks (before any store).
         asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-        w.store(it);
+        w.store(it, args.p.out.C, args.p.out.Z, args.p.out.planes);
         if (!more) break;
         it = next;
     }

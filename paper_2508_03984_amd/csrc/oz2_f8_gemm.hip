@@ -259,11 +259,22 @@ __global__ __launch_bounds__(256) void k_f8_ranges(F8Args p) {
     if (row >= p.m) return;
     const int col = (int)(id - row * per_row) * 4, valid = p.n - col;
     const F8Out &o = p.out;
-    const float *from = o.planes + row * o.ldp + col;
+    const float *const from = o.planes + row * o.ldp + col;
     f8_v4f s{0.f, 0.f, 0.f, 0.f}, t{0.f, 0.f, 0.f, 0.f};
-    for (int r = 0; r < p.ranges; ++r, from += o.plane) {
-        s += *reinterpret_cast<const f8_v4f *>(from);
-        if (GATED) t += *reinterpret_cast<const f8_v4f *>(from + o.ldp / 2);
+    for (int r0 = 0; r0 < p.ranges; r0 += 4) {                 // four loads at a time: one after the other costs a way to memory each
+        f8_v4f x[4], y[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float *const plane = from + (int64_t)min(r0 + r, p.ranges - 1) * o.plane;
+            x[r] = *reinterpret_cast<const f8_v4f *>(plane);
+            if (GATED) y[r] = *reinterpret_cast<const f8_v4f *>(plane + o.ldp / 2);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r0 + r < p.ranges) {
+                s += x[r];
+                if (GATED) t += y[r];
+            }
     }
     float x[4] = {s[0], s[1], s[2], s[3]};
     if constexpr (!GATED) f8_update_row<4>(o, row * o.ldc + col, x, valid);

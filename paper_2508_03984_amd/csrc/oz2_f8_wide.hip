@@ -342,7 +342,7 @@ struct Wide {
     }
     // 16 numbers of 16 bits of a row per lane, from four blocks of accumulators: rounded first, so that half as many words are exchanged.
     template <int TYPE>
-    static __device__ __forceinline__ void store_16_bits(uint16_t *to, const float (&x)[16]) {
+    static __device__ __forceinline__ void store_sixteen(uint16_t *to, const float (&x)[16]) {
         uint32_t lo[4], hi[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -353,10 +353,10 @@ struct Wide {
         const f8_v4i w[2] = {{l[0], h[0], l[1], h[1]}, {l[2], h[2], l[3], h[3]}};
         __builtin_memcpy(to, w, 32);                           // (wherever C lies)
     }
-    // The results of a whole tile in 16 bits.
+    // The results of a tile in 16 bits, C not read.  (Of a tile that was moved inwards, what the neighbour has is written twice, the same.)
     template <int TYPE>
-    __device__ __forceinline__ void store_whole(const Item &it, const F8Out &o, int up) const {
-        const int64_t row = it.tr * 256 + (wave >> 1) * 128 + lrow, col = it.tc * COLS + (wave & 1) * (COLS / 2) + quarter * 16;
+    __device__ __forceinline__ void store_16_bits(const F8Out &o, int64_t row0, int64_t col0, int up) const {
+        const int64_t row = row0 + (wave >> 1) * 128 + lrow, col = col0 + (wave & 1) * (COLS / 2) + quarter * 16;
         uint16_t *const c = static_cast<uint16_t *>(o.C) + row * o.ldc + col;
         uint16_t *const z = GATED ? static_cast<uint16_t *>(o.Z) + row * o.ldz + col : nullptr;
         static_for<8>([&](auto number) {
@@ -366,21 +366,30 @@ struct Wide {
             take<i, 4>(y);
             if constexpr (GATED) {
                 if (o.Z) {
-                    store_16_bits<TYPE>(z + i * 16 * o.ldz, x);
-                    store_16_bits<TYPE>(z + i * 16 * o.ldz + up, y);
+                    store_sixteen<TYPE>(z + i * 16 * o.ldz, x);
+                    store_sixteen<TYPE>(z + i * 16 * o.ldz + up, y);
                 }
                 f8_gated(x, y, o.act);
-                store_16_bits<TYPE>(c + i * 16 * o.ldc, x);
+                store_sixteen<TYPE>(c + i * 16 * o.ldc, x);
             } else {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) { x[e] *= o.alpha; y[e] *= o.alpha; }
-                store_16_bits<TYPE>(c + i * 16 * o.ldc, x);
-                store_16_bits<TYPE>(c + i * 16 * o.ldc + 64, y);
+                store_sixteen<TYPE>(c + i * 16 * o.ldc, x);
+                store_sixteen<TYPE>(c + i * 16 * o.ldc + 64, y);
             }
             __builtin_amdgcn_sched_barrier(0);
         });
     }
-    // The results of any tile, 16 rows at a time; this code exists once.
+    // The sums in binary32, 4 columns of a row per lane as they lie in the accumulators; gated, the second weight's `second` further.
+    __device__ __forceinline__ void store_sums(float *to, int64_t ld, int64_t row0, int64_t col0, int64_t second, float alpha) const {
+        float *const first = to + (row0 + (wave >> 1) * 128 + lrow) * ld + col0 + (wave & 1) * (COLS / 2) + quarter * 4;
+        static_for<64>([&](auto number) {
+            constexpr int i = decltype(number)::value / 8, j = decltype(number)::value % 8;
+            f8_v4f x{accumulator<32 * i + 4 * j>(), accumulator<32 * i + 4 * j + 1>(), accumulator<32 * i + 4 * j + 2>(), accumulator<32 * i + 4 * j + 3>()};
+            x *= alpha;
+            __builtin_memcpy(first + i * 16 * ld + (GATED ? j % 4 * 16 + (j / 4 ? second : 0) : j * 16), &x, 16);
+        });
+    }
     __device__ __forceinline__ void store(const Item &it, void *c, void *z, float *planes) const {
         const ArgsPtr a = arguments();
         F8Out o = fetch(&a->p.out);
@@ -389,11 +398,17 @@ struct Wide {
         o.planes = planes;
         const int m = a->p.m, n = a->p.n, up = a->p.up;
         const int row0 = min(it.tr * 256, m - 256), col0 = min(it.tc * COLS, n - COLS);
-        if (row0 == it.tr * 256 && col0 == it.tc * COLS && o.type != kF8F32 && o.beta == 0.0f && !o.planes) {
-            if (o.type == kF8Bf16) store_whole<kF8Bf16>(it, o, up);
-            else store_whole<kF8F16>(it, o, up);
+        if (o.planes) {
+            store_sums(o.planes + it.range * o.plane, o.ldp, row0, col0, o.ldp / 2, 1.0f);
             return;
         }
+        if (o.beta == 0.0f && (o.type != kF8F32 || !GATED)) {
+            if (o.type == kF8Bf16) store_16_bits<kF8Bf16>(o, row0, col0, up);
+            else if (o.type == kF8F16) store_16_bits<kF8F16>(o, row0, col0, up);
+            else store_sums(static_cast<float *>(o.C), o.ldc, row0, col0, 0, o.alpha);
+            return;
+        }
+        // Anything else, 16 rows at a time; this code exists once.
         const int first = row0 + (wave >> 1) * 128 + lrow;
 #pragma unroll 1
         for (int unit = 0; unit < 16; ++unit) {
@@ -412,18 +427,10 @@ struct Wide {
             const bool ours = row >= it.tr * 256 && from < 16;
             exchange(x);
             if constexpr (!GATED) {
-                if (!ours) continue;
-                if (o.planes) f8_store_row<16>(o.planes, kF8F32, it.range * o.plane + (int64_t)row * o.ldp + col, x, 16, from);
-                else f8_update_row<16>(o, (int64_t)row * o.ldc + col, x, 16, from);
+                if (ours) f8_update_row<16>(o, (int64_t)row * o.ldc + col, x, 16, from);
             } else {
                 exchange(u);
                 if (!ours) continue;
-                if (o.planes) {
-                    const int64_t at = it.range * o.plane + (int64_t)row * o.ldp + col;
-                    f8_store_row<16>(o.planes, kF8F32, at, x, 16, from);
-                    f8_store_row<16>(o.planes, kF8F32, at + o.ldp / 2, u, 16, from);
-                    continue;
-                }
                 if (o.Z) {
                     f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + col, x, 16, from);
                     f8_store_row<16>(o.Z, o.type, (int64_t)row * o.ldz + up + col, u, 16, from);

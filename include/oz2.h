@@ -322,7 +322,8 @@ oz2_status oz2_ctx_release(oz2_context *ctx);    /* frees what the context owns 
  * 2^-13 of the largest of the 8: a sum is off by less than 2^-10 sum |a||b|, for normal data by about 1.4e-5 of the norm of C.
  * The E4M3 numbers themselves are rounded at 2^-4.  Results are rounded to their type once.  The order of the sums depends on the sizes and on whether the
  * workspace has room for the planes of K ranges (oz2_f8_workspace_bytes), on nothing else: a call repeated gives the same bits.
- * NaN in an entry reaches the entries of C that it belongs to.  m == 0 or n == 0: nothing is done.  k up to 2^20.
+ * NaN in an entry reaches the entries of C that it belongs to.  m == 0 or n == 0: nothing is done.  k up to 2^20; m, n up to 2^30,
+ * and less where a launch would have 2^32 threads (OZ2_UNSUPPORTED).
  */
 typedef struct {
     void *q;

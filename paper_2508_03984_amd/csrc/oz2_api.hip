@@ -923,6 +923,7 @@ const char *oz2_status_string(oz2_status s) {
 namespace {
 
 constexpr int64_t kF8MaxRows = (int64_t)1 << 30, kF8MaxLd = (int64_t)1 << 23;
+constexpr int64_t kMaxThreads = (int64_t)1 << 32;              // of a launch, not reached
 
 // What the kernels rely on, for `rows` rows of k elements; *out is written if it holds.
 oz2_status f8_matrix(const oz2_f8 *x, int64_t k, F8Matrix *out) {
@@ -953,13 +954,15 @@ bool f8_numbers_ok(const void *p, int64_t ld, int64_t cols, int type) {
 oz2_status f8_sizes(int64_t m, int64_t n, int64_t k, int type, bool *nothing) {
     if (m < 0 || n < 0 || k < 0 || !f8_type_ok(type)) return OZ2_INVALID_ARG;
     *nothing = m == 0 || n == 0;
-    if (m > kF8MaxRows || n > kF8MaxRows || k > OZ2_MAX_K_BLOCKED || f8_tiles(m, 2 * n, 128) >= kF8MaxRows) return OZ2_UNSUPPORTED;
+    if (m > kF8MaxRows || n > kF8MaxRows || k > OZ2_MAX_K_BLOCKED) return OZ2_UNSUPPORTED;
     return OZ2_OK;
 }
 
 oz2_status f8_run(Ctx &g, F8Args &args, bool gated, hipStream_t stream) {
     std::lock_guard<std::mutex> lock(g.mu);
     F8Plan plan = f8_plan(args.m, args.n, args.k, gated);
+    const int64_t groups = plan.form == F8Form::kThin ? f8_ceil(args.n, 16) * 2 : f8_items(plan.form, args.m, args.n, gated) * plan.ranges;
+    if (groups * 256 >= kMaxThreads) return OZ2_UNSUPPORTED;
     if (plan.ranges > 1) {
         size_t have = 0, with_planes = 0;
         if (ensure_workspace(g, plan.plane_bytes, 0, &have, &with_planes) == OZ2_OK && with_planes >= plan.plane_bytes && g.ws) {
@@ -988,7 +991,7 @@ oz2_status oz2_f8_quantize(int64_t rows, int64_t cols, const void *X, int64_t ld
     F8Target out, turned;
     if (oz2_status st = f8_target(as_is, cols, &out)) return st;
     if (oz2_status st = f8_target(transposed, rows, &turned)) return st;
-    if (rows > kF8MaxRows || cols > kF8MaxRows || rows * f8_blocks(cols) >= kF8MaxRows) return OZ2_UNSUPPORTED;
+    if (rows > kF8MaxRows || cols > kF8MaxRows || rows * f8_blocks(cols) * 16 >= kMaxThreads || f8_blocks(rows) * f8_blocks(cols) * 512 >= kMaxThreads) return OZ2_UNSUPPORTED;
     const bool square = (as_is ? as_is : transposed)->block_rows != 1;
     OZ2_TRY(launch_f8_quantize(X, type, rows, cols, ldx, square, out, turned, stream));
     return OZ2_OK;
@@ -1050,6 +1053,7 @@ oz2_status oz2_f8_gated_grad(int64_t m, int64_t f, oz2_act act, const void *Z, i
     const int64_t up = f8_blocks(f) * kF8Block;
     if (!f8_numbers_ok(Z, ldz, up + f, type) || !f8_numbers_ok(dH, lddh, f, type)) return OZ2_INVALID_ARG;
     if ((D && D->block_rows != 1) || (DT && DT->block_rows != 1)) return OZ2_INVALID_ARG;
+    if (f8_blocks(m) * f8_blocks(f) * 1024 >= kMaxThreads) return OZ2_UNSUPPORTED;
     F8Target d, dt;
     if (oz2_status st = f8_target(D, up + f, &d)) return st;
     if (oz2_status st = f8_target(DT, m, &dt)) return st;

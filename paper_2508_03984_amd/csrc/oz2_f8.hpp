@@ -44,8 +44,8 @@ struct F8Args {
 };
 
 // ------------------------------------------------------------------ which kernel
-// kThin: few rows of A, B read once into registers (oz2_f8_thin.hip); the others tiles of 64, 128 (oz2_f8_gemm.hip) or 256 rows and
-// columns (oz2_f8_wide.hip), which may cut k into ranges whose sums are added by a second kernel.
+// kThin: few rows of A, B read once into registers (oz2_f8_thin.hip); the others tiles of C of 64 x 64, 64 x 128 (oz2_f8_gemm.hip) or
+// 256 x 256 (oz2_f8_wide.hip), which may cut k into ranges whose sums are added by a second kernel.
 enum class F8Form { kThin, kSmall, kMiddle, kLarge };
 struct F8Plan {
     F8Form form;
@@ -60,23 +60,28 @@ constexpr int kF8MaxRanges = 16;
 
 inline int64_t f8_blocks(int64_t k) { return (k + kF8Block - 1) / kF8Block; }
 inline int64_t f8_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t f8_tiles(int64_t rows, int64_t cols, int tile) { return f8_ceil(rows, tile) * f8_ceil(cols, tile); }
 // Columns of a plane: those of C, or of both sums; rows of a plane start at multiples of 64 bytes.
 inline int64_t f8_plane_ld(int64_t n, bool gated) { return f8_ceil(n, 16) * 16 * (gated ? 2 : 1); }
 
-// Of tiles of one size, what a call takes: so many microseconds once, and for each round of the compute units a time per tile and per block of k
-// (and, of both together, more where two small tiles share a unit).  Fitted to calls of 20 shapes from 65 x 8192 x 8192 to
-// 4096^3 in a graph, each with tiles of all sizes and with 1 to 16 ranges; off by 10 % mostly, 30 % at most.  Some, in us, tiles of 64 | 128 |
-// 256: 500 x 300 x 777 6.4 | 13.4 | 35; 512 x 4096 x 4096 18.8 | 27 | 38; 1024 x 4096 x 4096 33 | 28.8 | 46; 2048^3 20.6 | 17.6 | 28;
-// 3000^3 58 | 64 | 49; 4096 x 4096 x 512 31 | 30 | 19; 4096^3 121 | 102 | 62; with ranges: 65 x 8192 x 8192 24.2 -> 22.2 (2 ranges, tiles of
-// 64), 2048 x 2048 x 16384 90 (one, 128) -> 85 (4, 256), 1536 x 1000 x 40000 117 (2, 128) -> 84 (10, 256).
+// Tiles of C (gated: half as wide, since a tile has columns of both weights).
+inline int f8_tile_rows(F8Form form) { return form == F8Form::kLarge ? 256 : 64; }
+inline int f8_tile_cols(F8Form form) { return form == F8Form::kLarge ? 256 : form == F8Form::kMiddle ? 128 : 64; }
+inline int64_t f8_items(F8Form form, int64_t m, int64_t n, bool gated) { return f8_ceil(m, f8_tile_rows(form)) * f8_ceil(n, f8_tile_cols(form) / (gated ? 2 : 1)); }
+
+// What a call takes with tiles of one form, in us: something once, and for each round of the device a time per tile and per block of k.  A
+// round is `share` tiles on each of 256 units; in the last one, units with fewer tiles are faster per block.  Fitted to calls of 40
+// shapes from 65 x 8192 x 8192 to 4096^3 in a graph, each with all forms and with 1 to 16 ranges; off by 10 % mostly, by a third at most.
+// Some, 64 x 64 | 64 x 128 | 256 x 256: 500 x 300 x 777 6.3 | 8.8 | 20; 512 x 4096 x 4096 19 | - | 38; 2048^3 17.6 | 15.4 | 28;
+// 3000^3 52 | - | 39; 4096 x 4096 x 512 23 | 24 | 19; 4096^3 105 | - | 60; 8192 x 1024 x 256 10.7 | 12.3 | -; tiles of 128 x 128 were
+// behind one of these everywhere.  With ranges: 54 x 205 x 13245 22 (2) -> 9.4 (16), 2048 x 2048 x 16384 103 (one, 64 x 64) -> 74 (4, 256 x 256).
 struct F8Cost {
-    int tile, slots;
-    double once, per_tile, per_block;
+    F8Form form;
+    int share;
+    double once, per_tile, first_block, further_block;         // per block: the first tile of a unit, each further one
 };
-constexpr F8Cost kF8Costs[3] = {{64, 512, 3.5, 1.8, 0.40}, {128, 256, 4.0, 4.0, 0.64}, {256, 256, 13.0, 0.0, 1.55}};
-constexpr double kF8AlonePerBlock = 0.285;                     // a tile of 64 with a unit of its own
-constexpr double kF8RangesOnce = 3.0, kF8PlaneBytesPerUs = 3.2e6;   // the second kernel; planes are written and read
+constexpr F8Cost kF8Costs[3] = {{F8Form::kSmall, 4, 3.5, 2.2, 0.285, 0.125}, {F8Form::kMiddle, 2, 3.2, 2.8, 0.42, 0.18}, {F8Form::kLarge, 1, 9.0, 3.0, 1.45, 0.0}};
+constexpr double kF8LargeFewPerBlock = 1.1;                    // of at most 160 large tiles, which leave units to the others' power and caches
+constexpr double kF8RangesOnce = 3.0, kF8PlaneBytesPerUs = 4.0e6;   // the second kernel; planes are written and read
 constexpr double kF8BytesPerUs = 5.2e6;                        // from HBM
 
 // The form for few rows: one group of 4 blocks per wavefront at a time, B from HBM, A from the caches for every 16 columns.  In us, this form |
@@ -89,26 +94,27 @@ inline double f8_thin_us(int64_t m, int64_t n, int64_t k, bool gated) {
 
 inline F8Plan f8_plan(int64_t m, int64_t n, int64_t k, bool gated) {
     const int64_t wide = gated ? 2 * n : n, blocks = f8_blocks(k), groups = f8_ceil(blocks, 4);
-    F8Plan best{F8Form::kMiddle, 1, (int)std::max<int64_t>(blocks, 1), 0, 1e30};
+    F8Plan best{F8Form::kSmall, 1, (int)std::max<int64_t>(blocks, 1), 0, 1e30};
     if (m <= kF8ThinRows) {
         best.form = F8Form::kThin;
         best.us = f8_thin_us(m, n, k, gated);
     }
-    for (int f = 0; f < 3; ++f) {
-        const F8Cost &c = kF8Costs[f];
-        if (c.tile == 256 && (m < 256 || wide < 256)) continue;
-        const int64_t tiles = f8_ceil(m, c.tile) * f8_ceil(n, gated ? c.tile / 2 : c.tile);
+    for (const F8Cost &c : kF8Costs) {
+        if (c.form == F8Form::kLarge && (m < 256 || wide < 256)) continue;
+        const int64_t tiles = f8_items(c.form, m, n, gated), round = 256 * c.share;
         int64_t last = 0;
         for (int64_t asked = 1; asked <= std::min<int64_t>(std::max<int64_t>(groups, 1), kF8MaxRanges); ++asked) {
             const int64_t each = asked == 1 ? std::max<int64_t>(blocks, 1) : f8_ceil(groups, asked) * 4, ranges = std::max<int64_t>(f8_ceil(blocks, each), 1);
             if (ranges == last) continue;
             last = ranges;
-            if (c.tile == 256 && blocks - (ranges - 1) * each < kF8WideBlocks) continue;
-            const int64_t items = tiles * ranges, rounds = f8_ceil(items, c.slots);
-            const double per_block = f == 0 && items <= 256 ? kF8AlonePerBlock : c.per_block;
+            if (c.form == F8Form::kLarge && blocks - (ranges - 1) * each < kF8WideBlocks) continue;
+            const int64_t items = tiles * ranges, rounds = items / round, rest = f8_ceil(items - rounds * round, 256);
             const size_t planes = ranges == 1 ? 0 : (size_t)ranges * (size_t)m * (size_t)f8_plane_ld(n, gated) * 4;
-            const double us = std::max(c.once + rounds * (c.per_tile + each * per_block), 3.0 + (double)(m + wide) * k / kF8BytesPerUs) + (planes ? kF8RangesOnce + planes / kF8PlaneBytesPerUs : 0.0);
-            if (us < best.us) best = F8Plan{(F8Form)(f + 1), (int)ranges, (int)each, planes, us};
+            double us = c.once + rounds * (c.per_tile + each * (c.first_block + (c.share - 1) * c.further_block));
+            const double first = c.form == F8Form::kLarge && items <= 160 ? kF8LargeFewPerBlock : c.first_block;
+            if (rest) us += c.per_tile + each * (first + (rest - 1) * c.further_block);
+            us = std::max(us, 3.0 + (double)(m + wide) * k / kF8BytesPerUs) + (planes ? kF8RangesOnce + planes / kF8PlaneBytesPerUs : 0.0);
+            if (us < best.us) best = F8Plan{c.form, (int)ranges, (int)each, planes, us};
         }
     }
     return best;

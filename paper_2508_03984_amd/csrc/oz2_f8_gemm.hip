@@ -45,8 +45,8 @@ __device__ __forceinline__ void wait_ahead_and_meet(int ahead) {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int WM, int WN, int FM, int FN, int STAGES, bool GATED>
-__global__ __launch_bounds__(WM *WN * 64, STAGES == 2 ? 2 : 1) void k_f8_tiles(F8Args p, TileMap map) {
+template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, bool GATED>
+__global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_f8_tiles(F8Args p, TileMap map) {
     typedef F8Core<WM, WN, FM, FN, STAGES, GATED> C;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN, lrow = lane & 15, quarter = lane >> 4;
@@ -289,26 +289,32 @@ __global__ __launch_bounds__(256) void k_f8_ranges(F8Args p) {
     }
 }
 
-template <int WM, int WN, int FM, int FN, int STAGES, bool GATED>
+template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, bool GATED>
 hipError_t launch_tiles(const F8Args &args, hipStream_t stream) {
     typedef F8Core<WM, WN, FM, FN, STAGES, GATED> C;
     static thread_local int attr_device = -1;                // the attribute is per device (set again per thread: harmless)
     int dev = -1;
     if (hipError_t e = hipGetDevice(&dev)) return e;
     if (attr_device != dev) {
-        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_f8_tiles<WM, WN, FM, FN, STAGES, GATED>),
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_f8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, GATED>),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS_BYTES)) return e;
         attr_device = dev;
     }
     const int tiles_m = (args.m + C::BM - 1) / C::BM, tiles_n = (args.n + C::COLS - 1) / C::COLS;
     const TileMap map = make_tile_map(tiles_m, tiles_n, tiles_m * tiles_n * args.ranges);
-    hipLaunchKernelGGL((k_f8_tiles<WM, WN, FM, FN, STAGES, GATED>), dim3((unsigned)map.total), dim3(C::THREADS), C::LDS_BYTES, stream, args, map);
+    hipLaunchKernelGGL((k_f8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, GATED>), dim3((unsigned)map.total), dim3(C::THREADS), C::LDS_BYTES, stream, args, map);
     return hipGetLastError();
 }
 
+// Tiles of 64 x 64 by four wavefronts of 32 x 32, with four stages (two workgroups share a unit's LDS) while all tiles fit the device at
+// once and the way of a block to LDS counts, else with two (four workgroups); tiles of 64 x 128 with two stages.
 template <bool GATED>
 hipError_t launch_form(const F8Args &args, const F8Plan &plan, hipStream_t stream) {
-    if (hipError_t e = plan.form == F8Form::kLarge ? launch_f8_wide(args, GATED, stream) : plan.form == F8Form::kMiddle ? launch_tiles<2, 2, 4, 4, 4, GATED>(args, stream) : launch_tiles<2, 2, 2, 2, 4, GATED>(args, stream)) return e;
+    const bool deep = f8_items(plan.form, args.m, args.n, GATED) * args.ranges <= 512;
+    if (hipError_t e = plan.form == F8Form::kLarge    ? launch_f8_wide(args, GATED, stream)
+                       : plan.form == F8Form::kMiddle ? launch_tiles<2, 2, 2, 4, 2, 2, GATED>(args, stream)
+                       : deep                         ? launch_tiles<2, 2, 2, 2, 4, 2, GATED>(args, stream)
+                                                      : launch_tiles<2, 2, 2, 2, 2, 4, GATED>(args, stream)) return e;
     if (args.ranges == 1) return hipSuccess;
     const int64_t threads = (int64_t)args.m * ((args.n + 3) / 4);
     hipLaunchKernelGGL(k_f8_ranges<GATED>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, args);

@@ -79,3 +79,52 @@ def test_workspace_only_for_few_tiles_and_long_contractions(lib):
         for m, n, k in ((65, 17, 3000), (1500, 1111, 3001), (1536, 1000, 40000), (200, 1, 1 << 20)):
             wide = (n + 15) // 16 * 16 * (2 if gated else 1)
             assert need(m, n, k, gated) in [r * m * wide * 4 for r in (0, *range(2, 17))]
+
+
+def test_launches_that_would_be_too_large_are_refused(lib):
+    wide = f8(ld=1 << 20, ld_scale=1 << 13)
+    assert lib.oz2_f8_gemm(1 << 30, 1 << 20, 200, 1.0, f8(), f8(), 0.0, P, 1 << 20, 0, None) == UNSUPPORTED
+    assert lib.oz2_f8_gemm(1, 1 << 30, 200, 1.0, f8(), f8(), 0.0, P, 1 << 30, 0, None) == UNSUPPORTED
+    assert lib.oz2_f8_quantize(1 << 30, 200, P, 200, 0, f8(), None, None) == UNSUPPORTED
+    assert lib.oz2_f8_gated_grad(1 << 30, 1 << 19, 0, P, 1 << 20, P, 1 << 19, 0, wide, None, None) == UNSUPPORTED
+
+
+PLAN = r"""
+#include "%s"
+#include <cstdio>
+using namespace oz2;
+int main() {
+    long m, n, k; int gated;
+    while (scanf("%%ld %%ld %%ld %%d", &m, &n, &k, &gated) == 4) {
+        const F8Plan p = f8_plan(m, n, k, gated), q = f8_plan_one_range(m, n, k, gated);
+        printf("%%d %%d %%d %%zu %%d %%d\n", (int)p.form, p.ranges, p.kb_each, p.plane_bytes, (int)q.form, q.kb_each);
+    }
+}
+"""
+
+
+def test_plans_fit_what_the_kernels_assume(tmp_path):
+    """For many sizes: ranges are whole groups of 4 blocks, none empty, all blocks covered; the form for few rows has few rows; large tiles are
+    whole and have three blocks in every range; planes only for several ranges."""
+    import random
+    import subprocess
+    src, exe = tmp_path / "plan.cpp", tmp_path / "plan"
+    src.write_text(PLAN % os.path.join(os.path.dirname(oz.lib_path()), "csrc", "oz2_f8.hpp"))
+    subprocess.check_call(["g++", "-O1", "-std=c++17", str(src), "-o", str(exe)])
+    rng = random.Random(3)
+    size = lambda hi: int(2 ** rng.uniform(0, hi))  # noqa: E731
+    cases = [(size(15), size(15), size(20), rng.randrange(2)) for _ in range(4000)]
+    cases += [(m, n, k, g) for m in (1, 64, 65, 255, 256, 257) for n in (1, 127, 128, 129, 256, 60000) for k in (0, 1, 128, 257, 385, 512, 1 << 20) for g in (0, 1)]
+    out = subprocess.run([str(exe)], input="\n".join("%d %d %d %d" % c for c in cases), capture_output=True, text=True, check=True).stdout.split("\n")
+    forms = set()
+    for (m, n, k, gated), line in zip(cases, out):
+        form, ranges, each, planes, form1, each1 = map(int, line.split())
+        blocks, wide = -(-k // 128), n * (2 if gated else 1)
+        forms.add((form, ranges > 1))
+        assert 1 <= ranges <= 16 and (ranges - 1) * each < max(blocks, 1) <= ranges * max(each, 1)
+        assert ranges == 1 or each % 4 == 0
+        assert planes == (0 if ranges == 1 else ranges * m * (-(-n // 16) * 16) * (2 if gated else 1) * 4)
+        assert form != 0 or (m <= 64 and ranges == 1)
+        assert form != 3 or (m >= 256 and wide >= 256 and blocks - (ranges - 1) * each >= 3)
+        assert form1 == form and each1 == max(blocks, 1) and (form1 != 3 or blocks >= 3)
+    assert forms == {(0, False), (1, False), (1, True), (2, False), (2, True), (3, False), (3, True)}

@@ -84,12 +84,12 @@ constexpr double kF8LargeFewPerBlock = 1.1;                    // of at most 160
 constexpr double kF8RangesOnce = 3.0, kF8PlaneBytesPerUs = 4.0e6;   // the second kernel; planes are written and read
 constexpr double kF8BytesPerUs = 5.2e6;                        // from HBM
 
-// The form for few rows: one group of 4 blocks per wavefront at a time, B from HBM, A from the caches for every 16 columns.  In us, this form |
-// the best of the others: 1 x 8192 x 8192 13.7 | 16.2; 17 x 4096 x 4096 7.3 | 10.1; 33 x 2048 x 2048 5.9 | 7.3; 17 x 8192 x 8192 20.5 | 16.6;
-// 64 x 8192 x 8192 41.6 | 18.1.
+// The form for few rows: B from HBM, and what a unit's workgroups load through its caches, m rows of A and 16 or 32 of B for every 16 columns.
+// In us, this form | the best of the others: 1 x 8192 x 8192 13.7 | 16.2; 17 x 4096 x 4096 7.3 | 10.1; 33 x 2048 x 2048 5.9 | 7.3;
+// 23 x 84 x 11286 15.3 | 8.5; 60 x 84 x 4000 11.6 | 7.2; 17 x 8192 x 8192 20.5 | 16.6; 64 x 8192 x 8192 41.6 | 18.1.
 inline double f8_thin_us(int64_t m, int64_t n, int64_t k, bool gated) {
-    const double wide = gated ? 2.0 * n : n, steps = f8_ceil(f8_blocks(k), 4 * 8);
-    return std::max(1.0 + 2.5 * steps, 1.0 + wide * k / kF8BytesPerUs) + f8_ceil(n, 16) * (double)m * k / 9.4e6;
+    const double wide = gated ? 2.0 * n : n, shares = std::max(1.0, f8_ceil(n, 16) / 256.0);
+    return std::max(3.0 + shares * k * (m + (gated ? 32 : 16)) / 3.6e4, 1.0 + wide * k / kF8BytesPerUs);
 }
 
 inline F8Plan f8_plan(int64_t m, int64_t n, int64_t k, bool gated) {

@@ -350,8 +350,8 @@ struct Wide {
             hi[b] = F8Number<TYPE>::pack(x[4 * b + 2], x[4 * b + 3]);
         }
         const exchanged_t l = exchange_quarters(lo), h = exchange_quarters(hi);
-        const f8_v4i w[2] = {{l[0], h[0], l[1], h[1]}, {l[2], h[2], l[3], h[3]}};
-        __builtin_memcpy(to, w, 32);                           // (wherever C lies)
+        const uint32_t w[8] = {(uint32_t)l[0], (uint32_t)h[0], (uint32_t)l[1], (uint32_t)h[1], (uint32_t)l[2], (uint32_t)h[2], (uint32_t)l[3], (uint32_t)h[3]};
+        f8_store_words<8>(to, w);
     }
     // The results of a tile in 16 bits, C not read.  (Of a tile that was moved inwards, what the neighbour has is written twice, the same.)
     template <int TYPE>

@@ -8,7 +8,7 @@ import f8_reference as R
 
 torch = pytest.importorskip("torch")
 import paper_2508_03984_amd as oz  # noqa: E402
-from test_gpu_f8 import CUT, DTYPES, EPS, TINY, close, gated_case, host, random_f8  # noqa: E402
+from test_gpu_f8 import CUT, DTYPES, EPS, TINY, check_quantize, close, gated_case, host, random_f8, test_gated_grad as check_gated_grad  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,38 @@ def test_every_tile_of_a_large_product_with_odd_blocks():
     oz.oz2_f8_gemm(m, n, k, 1.0, A, B, 0.0, C, n)
     want = torch.from_numpy(a).cuda() @ torch.from_numpy(b).cuda().t()
     assert torch.equal(C.double(), want)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_end_anywhere(dtype, block_rows):
+    """Every number of numbers in the last piece of a row, and in rows shorter than a piece."""
+    rng = np.random.default_rng(17)
+    for cols in [*range(1, 26), *range(121, 146), 255, 257]:
+        for rows in (1, 5, 131):
+            x = np.clip(rng.standard_normal((rows, cols)) * np.exp(2 * rng.standard_normal((rows, cols))), -6e4, 6e4)
+            check_quantize(x, dtype, block_rows, spare_x=1, offset=cols % 2)
+
+
+@pytest.mark.parametrize("f", [3, 7, 8, 9, 15, 121, 127, 129, 135, 136])
+def test_gated_grad_of_rows_that_end_anywhere(f):
+    check_gated_grad(5, f, "bf16", f % 2)
+    check_gated_grad(129, f, "f32", f // 2 % 2)
+
+
+@pytest.mark.parametrize("m,n,k", [(6, 70, 300), (130, 71, 300), (257, 40000, 500), (3600, 3585, 400), (300, 201, 5000)])
+def test_adding_to_c(m, n, k):
+    """Rows of C that begin anywhere, in every form, with what is beside C left as it is."""
+    rng = np.random.default_rng(m + n)
+    (A, a), (B, b) = random_f8(rng, m, k, 1, 0, 0.3), random_f8(rng, n, k, 128, 0, 0.3)
+    want, mags = a @ b.T, np.abs(a) @ np.abs(b).T
+    for dtype, ldc in (("bf16", n + 1), ("f16", n + 2), ("f32", n + 3)):
+        before = torch.from_numpy(rng.standard_normal((m, ldc))).to("cuda", DTYPES[dtype])
+        before[:, n:] = float("nan")
+        C = before.clone()
+        oz.oz2_f8_gemm(m, n, k, 2.0, A, B, 0.25, C, ldc)
+        was = host(before[:, :n])
+        expect = 2.0 * want + 0.25 * was
+        err = np.abs(host(C[:, :n]) - expect)
+        assert (err <= 2 * CUT * mags + EPS[dtype] * (np.abs(expect) + 2 * CUT * mags) + 2.0 ** -22 * (2 * mags + np.abs(was)) + TINY[dtype]).all()
+        assert C[:, n:].isnan().all()

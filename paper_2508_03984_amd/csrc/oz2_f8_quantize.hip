@@ -62,37 +62,41 @@ struct Eight {
     f8_v4i w[kWords];
     typedef typename F8Number<TYPE>::T T;
     __device__ __forceinline__ void load(const T *from) { __builtin_memcpy(w, from, sizeof w); }
-    __device__ __forceinline__ void clear() { __builtin_memset(w, 0, sizeof w); }
-    // Of a row that ends at from[valid - 1] (`valid` may be negative).  A row of 8 or more numbers is read as its last 8, which are then moved
-    // down; number by number, one wait after the other, tiles at the edge took as long as all others (as they are, 16384 x 8191:
-    // 105 us instead of 78; the gradient's, 8192 x 8191, 256 instead of 173).
+    // Of a row that ends at from[valid - 1] (`valid` may be negative), to be followed by move_down(down(valid, eight)).  A row of 8 or more numbers
+    // (`eight`) is read as its last 8, which are then moved down; number by number, one wait after the other, tiles at the edge took as
+    // long as all others (as they are, 16384 x 8191: 105 us instead of 78; the gradient's, 8192 x 8191, 256 instead of 164).
     __device__ __forceinline__ void load(const T *from, int valid, bool eight) {
+        if (eight) {
+            load(from - max(8 - valid, 0));
+            return;
+        }
+        uint32_t words[4 * kWords];
+#pragma unroll
+        for (int i = 0; i < 4 * kWords; ++i) words[i] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) {
+                if constexpr (TYPE == kF8F32) words[i] = __builtin_bit_cast(uint32_t, from[i]);
+                else words[i / 2] |= (uint32_t)from[i] << (i % 2 * 16);
+            }
+#pragma unroll
+        for (int i = 0; i < 4 * kWords; ++i) w[i / 4][i % 4] = (int)words[i];
+    }
+    static __device__ __forceinline__ int down(int valid, bool eight) { return eight ? min(max(8 - valid, 0), 8) : 0; }
+    __device__ __forceinline__ void move_down(int by) {        // by 0 to 8 numbers, zeros following
         constexpr int N = 4 * kWords;
         uint32_t words[N];
-        if (eight) {
-            const int down = min(max(8 - valid, 0), 8);
-            load(from - max(8 - valid, 0));
 #pragma unroll
-            for (int i = 0; i < N; ++i) words[i] = (uint32_t)w[i / 4][i % 4];
+        for (int i = 0; i < N; ++i) words[i] = (uint32_t)w[i / 4][i % 4];
 #pragma unroll
-            for (int by = 1; by <= 8; by *= 2) {               // numbers
-                const bool move = down & by;
-                const int whole = by * N / 8;
+        for (int step = 1; step <= 8; step *= 2) {
+            const bool move = by & step;
+            const int whole = step * N / 8;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const uint32_t next = i + max(whole, 1) < N ? words[i + max(whole, 1)] : 0;
-                    words[i] = !move ? words[i] : whole ? next : __builtin_amdgcn_alignbyte(next, words[i], 2);
-                }
+            for (int i = 0; i < N; ++i) {
+                const uint32_t next = i + max(whole, 1) < N ? words[i + max(whole, 1)] : 0;
+                words[i] = !move ? words[i] : whole ? next : __builtin_amdgcn_alignbyte(next, words[i], 2);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) words[i] = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < valid) {
-                    if constexpr (TYPE == kF8F32) words[i] = __builtin_bit_cast(uint32_t, from[i]);
-                    else words[i / 2] |= (uint32_t)from[i] << (i % 2 * 16);
-                }
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) w[i / 4][i % 4] = (int)words[i];
@@ -112,6 +116,7 @@ constexpr int kTileThreads = 512, kTileWaves = kTileThreads / 64;
 constexpr int kOwn = 128 * 16 / kTileThreads;                  // rows of a thread
 
 // The rows of a thread of a tile, which has `rows` rows and `cols` columns; X at the tile's first number, with `before` more in front of it in its row.
+// settle_rows comes when all that a thread reads has been asked for: what it does at the edges waits for the numbers.
 template <int TYPE>
 __device__ __forceinline__ void load_rows(Eight<TYPE> (&in)[kOwn], const void *X, int64_t at, int64_t ld, int rows, int cols, int64_t before) {
     const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
@@ -121,11 +126,15 @@ __device__ __forceinline__ void load_rows(Eight<TYPE> (&in)[kOwn], const void *X
         for (int i = 0; i < kOwn; ++i) in[i].load(from + (kOwn * rg + i) * ld);
     } else {
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-            in[i].load(from + min(kOwn * rg + i, rows - 1) * ld, cols - 8 * cg, before + cols >= 8);
-            if (kOwn * rg + i >= rows) in[i].clear();
-        }
+        for (int i = 0; i < kOwn; ++i) in[i].load(from + min(kOwn * rg + i, rows - 1) * ld, cols - 8 * cg, before + cols >= 8);
     }
+}
+template <int TYPE>
+__device__ __forceinline__ void settle_rows(Eight<TYPE> (&in)[kOwn], int rows, int cols, int64_t before) {
+    if (rows == 128 && cols == 128) return;
+    const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) in[i].move_down(kOwn * rg + i < rows ? Eight<TYPE>::down(cols - 8 * cg, before + cols >= 8) : 8);
 }
 
 struct __align__(16) TileLds {
@@ -258,6 +267,7 @@ __global__ __launch_bounds__(kTileThreads) void k_f8_quantize_tiles(const void *
     const int here_r = (int)(rows - r0 < 128 ? rows - r0 : 128), here_c = (int)(cols - c0 < 128 ? cols - c0 : 128);
     Eight<TYPE> in[kOwn];
     load_rows<TYPE>(in, X, r0 * ldx + c0, ldx, here_r, here_c, c0);
+    settle_rows<TYPE>(in, here_r, here_c, c0);
     float x[kOwn][8];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) in[i].get(x[i]);
@@ -275,6 +285,7 @@ __global__ __launch_bounds__(256) void k_f8_quantize_rows(const void *X, int64_t
     float x[8], top = 0.0f;
     Eight<TYPE> in;
     in.load(static_cast<const typename Eight<TYPE>::T *>(X) + r * ldx + (int64_t)b * 128 + 8 * cg, here - 8 * cg, cols >= 8);
+    in.move_down(Eight<TYPE>::down(here - 8 * cg, cols >= 8));
     in.get(x);
 #pragma unroll
     for (int j = 0; j < 8; j += 2) top = max_magnitude(top, x[j], x[j + 1]);
@@ -312,6 +323,9 @@ __global__ __launch_bounds__(kTileThreads, 4) void k_f8_gated_grad(const void *Z
     load_rows<TYPE>(gate, Z, r0 * ldz + c0, ldz, here_r, here_c, c0);
     if (!part) load_rows<TYPE>(lift, Z, r0 * ldz + up + c0, ldz, here_r, here_c, c0);
     load_rows<TYPE>(grad, dH, r0 * ldh + c0, ldh, here_r, here_c, c0);
+    settle_rows<TYPE>(gate, here_r, here_c, c0);
+    if (!part) settle_rows<TYPE>(lift, here_r, here_c, c0);
+    settle_rows<TYPE>(grad, here_r, here_c, c0);
     float x[kOwn][8];
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {

@@ -307,7 +307,9 @@ hipError_t launch_tiles(const F8Args &args, hipStream_t stream) {
 }
 
 // Tiles of 64 x 64 by four wavefronts of 32 x 32, with four stages (two workgroups share a unit's LDS) while all tiles fit the device at
-// once and the way of a block to LDS counts, else with two (four workgroups); tiles of 64 x 128 with two stages.
+// once and the way of a block to LDS counts, else with two (four workgroups).  Four | two, us: 512 x 512 x 4096 13.6 | 18.8, 1400 x 1400 x 4096 (484
+// tiles) 18.8 | 21.1, 1500 x 1500 x 4096 (576) 28.0 | 22.1, 2000 x 1800 x 300 9.6 | 7.9.  Tiles of 64 x 128 with two stages.
+// 500 x 300 x 777 6.2 us, 1024^3 5.7 us, 2048^3 15.6 us (1.1 PFLOP/s): bound by the ways to memory and LDS one after the other, launch included.
 template <bool GATED>
 hipError_t launch_form(const F8Args &args, const F8Plan &plan, hipStream_t stream) {
     const bool deep = f8_items(plan.form, args.m, args.n, GATED) * args.ranges <= 512;

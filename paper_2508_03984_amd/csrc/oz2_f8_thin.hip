@@ -2,7 +2,8 @@
 // the matrix instruction, and C has no other work.  A workgroup takes 16 columns of C (gated: of both weights), its wavefronts
 // take groups of 4 blocks of k in turn and add their sums through LDS in ascending order.
 //
-// Bound: HBM (the bytes of B).
+// 1 x 8192 x 8192 13.7 us, 4.9 TB/s; 1 x 16384 x 16384 56 us, 4.8 TB/s; gated, 4 x 16384 x 4096 29.2 us, 4.6 TB/s.  Bound: HBM (the bytes of B);
+// with more rows what a compute unit reads through its caches, 16 bytes a lane from rows of their own (23 x 84 x 11286 15 us).
 #include "oz2_f8_device.hpp"
 
 namespace oz2 {

@@ -14,9 +14,11 @@
 //   - whole tiles of 16-bit results are rounded before the words change places among the lanes.
 // A workgroup per compute unit walks over the tiles; its requests run over the ends of tiles.  Every tile has at least kF8WideBlocks blocks.
 //
-// 8192 x 16384 x 16384: 1636 us, 2.69 PFLOP/s at 1.86 GHz under the power cap (on constant operands 1326 us, 3.32 PFLOP/s at 2.3 GHz; with
-// the loads taken out 1085).  By 8 wavefronts of 64 x 128, with a second set of wavefronts instead of the order by hand, 1725 (1546).
-// Bound: board power; beside it the loads, of which an L2 miss in six comes late.
+// 8192 x 16384 x 16384: 1510 to 1630 us, 2.9 to 2.7 PFLOP/s, on numbers of a normal distribution, at 1.8 to 1.9 GHz under the power cap; on constant operands 1350 us, 3.26 PFLOP/s at 2.3 GHz; with the loads taken
+// out 1085.  The matrix cores are busy 69 % of the cycles.  By 8 wavefronts of 64 x 128, with a second set of wavefronts instead of the order by
+// hand, 1725 (1546).  Bound: board power; beside it the loads, of which an L2 miss in six comes late, and what lies between
+// two tiles, for which there are no registers beside the next one's sums (8192 x 16384 at k = 4096 420 us, 4096 x 8192 at k = 16384 with as many
+// operations 389; gated, 8192 x 8192 x 4096 408, with its sums kept 450).
 #include <type_traits>
 #include <utility>
 

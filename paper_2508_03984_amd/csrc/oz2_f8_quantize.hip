@@ -5,7 +5,7 @@
 //
 // A block of one row for the matrix as it is and for its transpose, or of 128 x 128 for both, come from one read: a workgroup
 // holds a tile of 128 x 128 in registers, 4 x 8 numbers per thread, and turns the bytes of the transpose through LDS.
-// 16384 x 8192 bf16, as it is and transposed: 110 us, 4.9 TB/s (blocks of 128 x 128 108); as it is only, by rows, 71 us, 5.7 TB/s; 1500 x 1111 f32
+// 16384 x 8192 bf16, as it is and transposed: 110 us, 4.9 TB/s (blocks of 128 x 128 108); as it is only 71 to 79 us, 5.1 to 5.7 TB/s; 1500 x 1111 f32
 // 5.8 us, 64 x 8192 2.9 us.  Bound: HBM; the smallest calls by latency.
 #include "oz2_f8_device.hpp"
 
@@ -353,7 +353,10 @@ template <int TYPE>
 hipError_t launch_quantize(const void *X, int64_t rows, int64_t cols, int64_t ldx, bool square, const F8Target &as_is, const F8Target &transposed,
                            hipStream_t stream) {
     const int tiles_m = (int)((rows + 127) / 128), tiles_n = (int)((cols + 127) / 128);
-    if (!square && !transposed.q) {
+    // Blocks of one row as they are: by rows, unless whole tiles fill the device twice and are nearly all.  Rows | tiles, us, bf16: 1 x 8192 2.2 | 3.2, 1000 x 1111 2.6 | 3.9,
+    // 140 x 65536 6.0 | 7.0, 1000 x 8191 5.5 | 5.8, 2048 x 4096 5.6 | 4.7, 4096 x 4096 10.5 | 9.2, 16384 x 8192 74 to 79 | 75.
+    const bool by_tiles = rows / 128 * tiles_n >= 512 && 8 * (rows / 128) >= 7 * tiles_m;
+    if (!square && !transposed.q && !by_tiles) {
         const int64_t units = rows * tiles_n;
         hipLaunchKernelGGL((k_f8_quantize_rows<TYPE>), dim3((unsigned)((units + 15) / 16)), dim3(256), 0, stream, X, rows, cols, ldx, tiles_n, make_divisor(tiles_n), as_is);
     } else if (square) {

@@ -121,3 +121,14 @@ def test_adding_to_c(m, n, k):
         err = np.abs(host(C[:, :n]) - expect)
         assert (err <= 2 * CUT * mags + EPS[dtype] * (np.abs(expect) + 2 * CUT * mags) + 2.0 ** -22 * (2 * mags + np.abs(was)) + TINY[dtype]).all()
         assert C[:, n:].isnan().all()
+
+
+@pytest.mark.parametrize("rows,cols", [(2050, 4097), (1930, 4100), (1300, 200)])
+def test_quantize_as_it_is_by_rows_and_by_tiles(rows, cols):
+    """Matrices on both sides of the size from which tiles convert what is not transposed."""
+    rng = np.random.default_rng(rows)
+    X = torch.from_numpy(rng.standard_normal((rows, cols)) * np.exp(2 * rng.standard_normal((rows, cols)))).clamp(-6e4, 6e4).to("cuda", torch.bfloat16)
+    a = oz.F8.empty(rows, cols)
+    oz.oz2_f8_quantize(rows, cols, X, cols, a, None)
+    q, scale = R.quantize(host(X), 1)
+    assert np.array_equal(host(a.scale), scale) and np.array_equal(host(a.q), q)

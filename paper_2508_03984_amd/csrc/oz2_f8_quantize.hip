@@ -12,11 +12,12 @@
 namespace oz2 {
 namespace {
 
-// max(top, |x|, |y|) in one instruction.  A quiet NaN is passed over; an infinity or a signalling NaN leaves something that is not
-// below infinity, and then the maxima are taken again with finite_magnitude.
+// The largest of top, |x| and |y| in one instruction, NaN if one of them is.  (v_max3_f32 passes over NaN, and having met a signalling one it
+// has forgotten what came before.)  Whatever is not below infinity at the end has met NaN or an infinity, and then the maxima are taken
+// again with finite_magnitude.
 __device__ __forceinline__ float max_magnitude(float top, float x, float y) {
     float r;
-    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(top), "v"(x), "v"(y));
+    asm("v_maximum3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(top), "v"(x), "v"(y));
     return r;
 }
 __device__ __forceinline__ float finite_magnitude(float x) {

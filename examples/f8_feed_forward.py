@@ -63,11 +63,13 @@ class FeedForward:
         self.gate_up.master[:hidden].normal_(0, width ** -0.5, generator=gen)
         self.gate_up.master[self.up:].normal_(0, width ** -0.5, generator=gen)
         self.down.master.normal_(0, hidden ** -0.5, generator=gen)
-        self.ctx = oz.oz2_create()                            # the products' workspace, kept between calls
+        # The products' memory, kept between calls and where it is: what a captured graph holds stays valid when later calls need more.  Training
+        # and all servers of the block share it, so their calls and replays are ordered, on one stream or by events.
+        self.ctx = oz.oz2_create()
         self.convert()
 
     def close(self):
-        """Frees the workspace.  No graph that was captured with the block may run after it."""
+        """Frees the products' memory.  No graph that was captured with the block may run after it."""
         oz.oz2_destroy(self.ctx)
 
     def weights(self):
@@ -126,7 +128,7 @@ class Server:
         self.x = torch.zeros(tokens, block.width, dtype=torch.bfloat16, device="cuda")
         self.a = Activations(tokens, block.width, block.hidden, False)
         self.y = self.a.y
-        block.forward(self.x, self.a)                         # the workspace grows before the capture, not in it
+        block.forward(self.x, self.a)                         # memory is allocated before the capture, not in it
         torch.cuda.synchronize()
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):

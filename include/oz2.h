@@ -32,9 +32,9 @@
  *     launches anything;
  *   - inputs must be finite.  Inf/NaN inputs give an unspecified (but memory
  *     safe) result: the paper does not define them;
- *   - no entry point throws; besides the workspace growth above only oz2_destroy,
- *     oz2_release, oz2_set_workspace and oz2_last_stage_times_ms (and their oz2_ctx_
- *     forms) synchronise the device.
+ *   - no entry point throws; besides the workspace growth above (and hipMalloc for the planes of 8-bit
+ *     floating-point products, see oz2_f8_workspace_bytes) only oz2_destroy, oz2_release,
+ *     oz2_set_workspace and oz2_last_stage_times_ms (and their oz2_ctx_ forms) synchronise the device.
  */
 #ifndef OZ2_H
 #define OZ2_H
@@ -378,8 +378,12 @@ oz2_status oz2_f8_gated_grad(int64_t m, int64_t f, oz2_act act, const void *Z, i
 
 /*
  * Workspace of oz2_f8_gemm (gated = 0) and oz2_f8_gated (gated != 0, n = f): planes for the K ranges of a product with few tiles
- * and a long contraction, 0 for all others.  The library's own workspace grows for them as for any product; a caller's buffer, or a
- * limit, that has no room for them serves the call with one range (slower, and the sums in another order).
+ * and a long contraction, 0 for all others.  In a caller's buffer they lie in it.  Otherwise the context has memory of its own for them, beside its
+ * workspace: hipMalloc in the first call that needs so much, and never moved or freed before oz2_destroy, oz2_release or oz2_set_workspace, so that a
+ * captured graph may hold it whatever calls come later (all of it together is less than four times the largest planes on a device, and 4 MiB).  Where a caller's buffer
+ * or a limit has no room, or the memory is not to be had, the call is served with one range (slower, and the sums in another order).  A limit holds for the
+ * workspace and the planes together; a product whose workspace has to grow under it frees the planes first if they leave it no room.  A call that
+ * needs memory for planes inside a capture that allows none to be allocated returns OZ2_HIP_ERROR.
  */
 size_t oz2_f8_workspace_bytes(int64_t m, int64_t n, int64_t k, int gated);
 

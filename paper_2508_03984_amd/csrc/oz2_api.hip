@@ -16,6 +16,14 @@
 #include "oz2_kernels.hpp"
 #include "oz2_plan.hpp"
 
+// Memory for the planes of K ranges of 8-bit floating-point products (f8_planes).
+struct F8Planes {
+    char *ptr;
+    size_t bytes;
+    int device;
+};
+constexpr int kMaxF8Planes = 64;
+
 // Everything a product call keeps between its launches and for the diagnostics that follow it:
 // one workspace, the options, the events of the per-stage timing and the second stream of the
 // overlapped form.  Calls on one context share its workspace, so they must be ordered by the
@@ -27,7 +35,9 @@ struct oz2_context {
     size_t ws_planes = 0;                  // of them (library's own buffer): reserve for the planes of K ranges
     bool ws_owned = false;
     int ws_device = -1;                    // device of the library's own buffer
-    size_t ws_limit = 0;                   // for the library's own buffer; 0 = none
+    F8Planes f8_planes[kMaxF8Planes];      // apart from ws, in the order in which they were allocated
+    int n_f8_planes = 0;
+    size_t ws_limit = 0;                   // for the library's own buffers; 0 = none
     oz2::Layout last{};
     oz2::Panels last_panels{0, 0, 0};
     int64_t last_gemm_launches = 0;        // INT8 GEMM launches of the products of the last call
@@ -62,6 +72,26 @@ Ctx &default_context() {
 }
 inline Ctx &resolve(oz2_context *c) { return c ? *c : default_context(); }
 
+size_t held_by_f8(const Ctx &g) {
+    size_t sum = 0;
+    for (int i = 0; i < g.n_f8_planes; ++i) sum += g.f8_planes[i].bytes;
+    return sum;
+}
+
+// Waits for the devices that may still use them.
+void free_f8_planes(Ctx &g) {
+    if (g.n_f8_planes == 0) return;
+    int dev = -1;
+    const bool known = hipGetDevice(&dev) == hipSuccess;
+    for (int i = 0; i < g.n_f8_planes; ++i) {
+        (void)hipSetDevice(g.f8_planes[i].device);
+        (void)hipDeviceSynchronize();
+        (void)hipFree(g.f8_planes[i].ptr);
+    }
+    if (known) (void)hipSetDevice(dev);
+    g.n_f8_planes = 0;
+}
+
 // Makes at least `need_min` bytes of workspace available, `need_whole` if nothing limits it;
 // *have receives the bytes the call may use, *with_planes the same with what there is behind them for the planes of K ranges (a
 // caller's buffer: all of it).  Growing the library's own buffer (or moving it to
@@ -94,7 +124,10 @@ oz2_status ensure_workspace(Ctx &g, size_t need_whole, size_t need_min, size_t *
         }
         void *p = nullptr;
         size_t planes = planes_reserve(want);
-        if (g.ws_limit) planes = std::min(planes, g.ws_limit - want);
+        if (g.ws_limit) {
+            if (held_by_f8(g) > g.ws_limit - want) free_f8_planes(g);
+            planes = std::min(planes, g.ws_limit - want - held_by_f8(g));
+        }
         if (planes > 0 && hipMalloc(&p, want + planes) != hipSuccess) {
             (void)hipGetLastError();                          // no later success clears it, and the check after a launch would find it
             p = nullptr;
@@ -491,6 +524,7 @@ void release_workspace(Ctx &g) {                           // g.mu is held
         (void)hipFree(g.ws);
     }
     g.ws = nullptr; g.ws_bytes = g.ws_planes = 0; g.ws_owned = false; g.have_last = g.have_last_prod = false;
+    free_f8_planes(g);
     drop_device_resources(g);
     g.res_device = -1;
 }
@@ -581,6 +615,7 @@ oz2_status oz2_ctx_set_workspace(oz2_context *ctx, void *dev_ptr, size_t bytes) 
         if (hipDeviceSynchronize() != hipSuccess) return OZ2_HIP_ERROR;
         (void)hipFree(g.ws);
     }
+    free_f8_planes(g);
     g.ws = static_cast<char *>(dev_ptr);
     g.ws_bytes = dev_ptr ? bytes : 0;
     g.ws_planes = 0;
@@ -958,16 +993,54 @@ oz2_status f8_sizes(int64_t m, int64_t n, int64_t k, int type, bool *nothing) {
     return OZ2_OK;
 }
 
+// Memory for `bytes` of planes; *out is null if there is no room.  They are not part of the workspace: that would have to grow for
+// them, and what it had before, the last product's stages or what a captured graph replays into, would be gone.  For the same reason no buffer
+// of planes is freed while the context keeps its memory: more of them are allocated, each at least twice as large as the largest before where that is to be
+// had, and a call takes the first with room, so that one that has run finds the same again.
+oz2_status f8_planes(Ctx &g, size_t bytes, float **out) {
+    *out = nullptr;
+    if (g.ws && !g.ws_owned) {                                 // a caller's buffer: nothing is allocated beside it
+        if (g.ws_bytes < bytes) return OZ2_OK;
+        g.have_last = g.have_last_prod = false;                // the stages of the product before are overwritten
+        *out = reinterpret_cast<float *>(g.ws);
+        return OZ2_OK;
+    }
+    if (g.ws_limit && bytes > g.ws_limit) return OZ2_OK;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return OZ2_HIP_ERROR;
+    size_t largest = 0;
+    for (int i = 0; i < g.n_f8_planes; ++i) {
+        const F8Planes &p = g.f8_planes[i];
+        if (p.device != dev) continue;
+        if (p.bytes >= bytes) { *out = reinterpret_cast<float *>(p.ptr); return OZ2_OK; }
+        largest = std::max(largest, p.bytes);
+    }
+    if (g.n_f8_planes == kMaxF8Planes) return OZ2_OK;
+    constexpr size_t kGrain = (size_t)2 << 20;
+    const size_t held = g.ws_bytes + held_by_f8(g);
+    for (const size_t ask : {std::max((bytes + kGrain - 1) / kGrain * kGrain, 2 * largest), bytes}) {
+        if (g.ws_limit && (held > g.ws_limit || ask > g.ws_limit - held)) continue;
+        void *p = nullptr;
+        const hipError_t e = hipMalloc(&p, ask);
+        if (e == hipSuccess) {
+            g.f8_planes[g.n_f8_planes++] = F8Planes{static_cast<char *>(p), ask, dev};
+            *out = static_cast<float *>(p);
+            return OZ2_OK;
+        }
+        (void)hipGetLastError();                               // (the check after a launch would find it)
+        if (e != hipErrorOutOfMemory) return OZ2_HIP_ERROR;    // a stream is being captured, say
+    }
+    return OZ2_OK;
+}
+
 oz2_status f8_run(Ctx &g, F8Args &args, bool gated, hipStream_t stream) {
     std::lock_guard<std::mutex> lock(g.mu);
     F8Plan plan = f8_plan(args.m, args.n, args.k, gated);
     const int64_t groups = plan.form == F8Form::kThin ? f8_ceil(args.n, 16) * 2 : f8_items(plan.form, args.m, args.n, gated) * plan.ranges;
     if (groups * 256 >= kMaxThreads) return OZ2_UNSUPPORTED;
     if (plan.ranges > 1) {
-        size_t have = 0, with_planes = 0;
-        if (ensure_workspace(g, plan.plane_bytes, 0, &have, &with_planes) == OZ2_OK && with_planes >= plan.plane_bytes && g.ws) {
-            g.have_last = g.have_last_prod = false;            // the stages of the product before are overwritten
-            args.out.planes = reinterpret_cast<float *>(g.ws);
+        if (oz2_status st = f8_planes(g, plan.plane_bytes, &args.out.planes)) return st;
+        if (args.out.planes) {
             args.out.ldp = f8_plane_ld(args.n, gated);
             args.out.plane = (int64_t)args.m * args.out.ldp;
         } else plan = f8_plan_one_range(args.m, args.n, args.k, gated);

@@ -119,6 +119,7 @@ oz2_status ensure_workspace(Ctx &g, size_t need_whole, size_t need_min, size_t *
             const hipError_t e = hipDeviceSynchronize();
             (void)hipFree(g.ws);
             g.ws = nullptr; g.ws_bytes = g.ws_planes = 0;
+            g.have_last = g.have_last_prod = false;           // the stages went with it, also if nothing takes its place
             if (elsewhere && hipSetDevice(dev) != hipSuccess) return OZ2_HIP_ERROR;
             if (e != hipSuccess) return OZ2_HIP_ERROR;
         }

@@ -1065,8 +1065,10 @@ oz2_status oz2_f8_quantize(int64_t rows, int64_t cols, const void *X, int64_t ld
     F8Target out, turned;
     if (oz2_status st = f8_target(as_is, cols, &out)) return st;
     if (oz2_status st = f8_target(transposed, rows, &turned)) return st;
-    if (rows > kF8MaxRows || cols > kF8MaxRows || rows * f8_blocks(cols) * 16 >= kMaxThreads || f8_blocks(rows) * f8_blocks(cols) * 512 >= kMaxThreads) return OZ2_UNSUPPORTED;
     const bool square = (as_is ? as_is : transposed)->block_rows != 1;
+    if (rows > kF8MaxRows || cols > kF8MaxRows) return OZ2_UNSUPPORTED;
+    const int64_t threads = f8_by_rows(rows, cols, square, transposed) ? f8_row_groups(rows, cols) * kF8RowThreads : f8_tile_groups(rows, cols) * kF8TileThreads;
+    if (threads >= kMaxThreads) return OZ2_UNSUPPORTED;
     OZ2_TRY(launch_f8_quantize(X, type, rows, cols, ldx, square, out, turned, stream));
     return OZ2_OK;
 }
@@ -1127,7 +1129,7 @@ oz2_status oz2_f8_gated_grad(int64_t m, int64_t f, oz2_act act, const void *Z, i
     const int64_t up = f8_blocks(f) * kF8Block;
     if (!f8_numbers_ok(Z, ldz, up + f, type) || !f8_numbers_ok(dH, lddh, f, type)) return OZ2_INVALID_ARG;
     if ((D && D->block_rows != 1) || (DT && DT->block_rows != 1)) return OZ2_INVALID_ARG;
-    if (f8_blocks(m) * f8_blocks(f) * 1024 >= kMaxThreads) return OZ2_UNSUPPORTED;
+    if (f8_grad_groups(m, f) * kF8TileThreads >= kMaxThreads) return OZ2_UNSUPPORTED;
     F8Target d, dt;
     if (oz2_status st = f8_target(D, up + f, &d)) return st;
     if (oz2_status st = f8_target(DT, m, &dt)) return st;

@@ -128,6 +128,19 @@ inline F8Plan f8_plan_one_range(int64_t m, int64_t n, int64_t k, bool gated) {
     return p;
 }
 
+// ------------------------------------------------------------------ conversions
+// Blocks of one row as they are: by rows, unless whole tiles fill the device twice and are nearly all.  Rows | tiles, us, bf16: 1 x 8192 2.2 | 3.2, 1000 x 1111 2.6 | 3.9,
+// 140 x 65536 6.0 | 7.0, 1000 x 8191 5.5 | 5.8, 2048 x 4096 5.6 | 4.7, 4096 x 4096 10.5 | 9.2, 16384 x 8192 74 to 79 | 75.
+inline bool f8_by_rows(int64_t rows, int64_t cols, bool square, bool transposed) {
+    const bool by_tiles = rows / kF8Block * f8_blocks(cols) >= 512 && 8 * (rows / kF8Block) >= 7 * f8_blocks(rows);
+    return !square && !transposed && !by_tiles;
+}
+// Workgroups: by rows 16 blocks of 128 each, otherwise a tile of 128 x 128; of the gated block's gradient one of its two parts, by turns of 8 tiles.
+constexpr int kF8RowThreads = 256, kF8TileThreads = 512;
+inline int64_t f8_row_groups(int64_t rows, int64_t cols) { return f8_ceil(rows * f8_blocks(cols), 16); }
+inline int64_t f8_tile_groups(int64_t rows, int64_t cols) { return f8_blocks(rows) * f8_blocks(cols); }
+inline int64_t f8_grad_groups(int64_t m, int64_t f) { return f8_ceil(f8_tile_groups(m, f), 8) * 16; }
+
 #if defined(__HIPCC__)
 hipError_t launch_f8_product(const F8Args &args, const F8Plan &plan, bool gated, hipStream_t stream);
 hipError_t launch_f8_wide(const F8Args &args, bool gated, hipStream_t stream);

@@ -114,7 +114,7 @@ struct Eight {
     }
 };
 
-constexpr int kTileThreads = 512, kTileWaves = kTileThreads / 64;
+constexpr int kTileThreads = kF8TileThreads, kTileWaves = kTileThreads / 64;
 constexpr int kOwn = 128 * 16 / kTileThreads;                  // rows of a thread
 
 // The rows of a thread of a tile, which has `rows` rows and `cols` columns; X at the tile's first number, with `before` more in front of it in its row.
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(kTileThreads) void k_f8_quantize_tiles(const void *
 
 // Blocks of one row, as they are: 16 lanes take a block, 8 numbers each.
 template <int TYPE>
-__global__ __launch_bounds__(256) void k_f8_quantize_rows(const void *X, int64_t rows, int64_t cols, int64_t ldx, int blocks, Divisor by_row, F8Target out) {
+__global__ __launch_bounds__(kF8RowThreads) void k_f8_quantize_rows(const void *X, int64_t rows, int64_t cols, int64_t ldx, int blocks, Divisor by_row, F8Target out) {
     const int unit = (int)blockIdx.x * 16 + (threadIdx.x >> 4), cg = threadIdx.x & 15;
     const int r = divide(unit, by_row), b = unit - r * blocks;
     if (r >= rows) return;
@@ -353,17 +353,14 @@ __global__ __launch_bounds__(kTileThreads, 4) void k_f8_gated_grad(const void *Z
 template <int TYPE>
 hipError_t launch_quantize(const void *X, int64_t rows, int64_t cols, int64_t ldx, bool square, const F8Target &as_is, const F8Target &transposed,
                            hipStream_t stream) {
-    const int tiles_m = (int)((rows + 127) / 128), tiles_n = (int)((cols + 127) / 128);
-    // Blocks of one row as they are: by rows, unless whole tiles fill the device twice and are nearly all.  Rows | tiles, us, bf16: 1 x 8192 2.2 | 3.2, 1000 x 1111 2.6 | 3.9,
-    // 140 x 65536 6.0 | 7.0, 1000 x 8191 5.5 | 5.8, 2048 x 4096 5.6 | 4.7, 4096 x 4096 10.5 | 9.2, 16384 x 8192 74 to 79 | 75.
-    const bool by_tiles = rows / 128 * tiles_n >= 512 && 8 * (rows / 128) >= 7 * tiles_m;
-    if (!square && !transposed.q && !by_tiles) {
-        const int64_t units = rows * tiles_n;
-        hipLaunchKernelGGL((k_f8_quantize_rows<TYPE>), dim3((unsigned)((units + 15) / 16)), dim3(256), 0, stream, X, rows, cols, ldx, tiles_n, make_divisor(tiles_n), as_is);
+    const int tiles_n = (int)f8_blocks(cols);
+    const dim3 tiles((unsigned)f8_tile_groups(rows, cols));
+    if (f8_by_rows(rows, cols, square, transposed.q != nullptr)) {
+        hipLaunchKernelGGL((k_f8_quantize_rows<TYPE>), dim3((unsigned)f8_row_groups(rows, cols)), dim3(kF8RowThreads), 0, stream, X, rows, cols, ldx, tiles_n, make_divisor(tiles_n), as_is);
     } else if (square) {
-        hipLaunchKernelGGL((k_f8_quantize_tiles<TYPE, true>), dim3((unsigned)(tiles_m * tiles_n)), dim3(kTileThreads), 0, stream, X, rows, cols, ldx, tiles_n, make_divisor(tiles_n), as_is, transposed);
+        hipLaunchKernelGGL((k_f8_quantize_tiles<TYPE, true>), tiles, dim3(kTileThreads), 0, stream, X, rows, cols, ldx, tiles_n, make_divisor(tiles_n), as_is, transposed);
     } else {
-        hipLaunchKernelGGL((k_f8_quantize_tiles<TYPE, false>), dim3((unsigned)(tiles_m * tiles_n)), dim3(kTileThreads), 0, stream, X, rows, cols, ldx, tiles_n, make_divisor(tiles_n), as_is, transposed);
+        hipLaunchKernelGGL((k_f8_quantize_tiles<TYPE, false>), tiles, dim3(kTileThreads), 0, stream, X, rows, cols, ldx, tiles_n, make_divisor(tiles_n), as_is, transposed);
     }
     return hipGetLastError();
 }
@@ -371,10 +368,9 @@ hipError_t launch_quantize(const void *X, int64_t rows, int64_t cols, int64_t ld
 template <int TYPE>
 hipError_t launch_grad(const void *Z, int64_t ldz, const void *dH, int64_t ldh, int64_t m, int64_t f, int64_t up, int act, const F8Target &D,
                        const F8Target &DT, hipStream_t stream) {
-    const int tiles_m = (int)((m + 127) / 128), tiles_n = (int)((f + 127) / 128);
-    const int tiles = tiles_m * tiles_n;
-    hipLaunchKernelGGL((k_f8_gated_grad<TYPE>), dim3((unsigned)((tiles + 7) / 8 * 16)), dim3(kTileThreads), 0, stream, Z, ldz, dH, ldh, m, f, up, act, tiles,
-                       tiles_n, make_divisor(tiles_n), D, DT);
+    const int tiles_n = (int)f8_blocks(f), tiles = (int)f8_tile_groups(m, f);
+    hipLaunchKernelGGL((k_f8_gated_grad<TYPE>), dim3((unsigned)f8_grad_groups(m, f)), dim3(kTileThreads), 0, stream, Z, ldz, dH, ldh, m, f, up, act, tiles, tiles_n,
+                       make_divisor(tiles_n), D, DT);
     return hipGetLastError();
 }
 

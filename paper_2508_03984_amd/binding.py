@@ -619,8 +619,8 @@ class F8:
             raise ValueError(f"scale of {-(-rows // block_rows)} x {-(-cols // 128)} blocks expected, got {tuple(scale.shape)}")
         if (cols > 1 and q.stride(1) != 1) or (scale.shape[1] > 1 and scale.stride(1) != 1):
             raise ValueError("row-major q and scale expected")
-        ld = q.stride(0) if rows > 1 else max(q.stride(0), _up(cols, 16))
-        ld_scale = scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), _up(scale.shape[1], 4))
+        ld = q.stride(0) if rows > 1 else _up(cols, 16)       # (of one row the stride says nothing)
+        ld_scale = scale.stride(0) if scale.shape[0] > 1 else _up(scale.shape[1], 4)
         for t, row, unit in ((q, cols, 16), (scale, scale.shape[1], 4)):        # the last row is stored whole, too
             left = t.untyped_storage().nbytes() - t.storage_offset() - (t.shape[0] - 1) * t.stride(0)
             if t.numel() and left < _up(row, unit):

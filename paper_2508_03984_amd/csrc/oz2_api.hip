@@ -1086,7 +1086,7 @@ oz2_status oz2_ctx_f8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, fl
     }
     args.m = (int)m; args.n = (int)n; args.k = (int)k;
     args.out.C = C; args.out.ldc = ldc; args.out.type = type;
-    args.out.alpha = alpha; args.out.beta = beta;
+    args.out.alpha = k > 0 ? alpha : 0.0f; args.out.beta = beta;          // (no sum: no infinity or NaN from it either)
     return f8_run(resolve(ctx), args, false, stream);
 }
 

@@ -84,12 +84,16 @@ constexpr double kF8LargeFewPerBlock = 1.1;                    // of at most 160
 constexpr double kF8RangesOnce = 3.0, kF8PlaneBytesPerUs = 4.0e6;   // the second kernel; planes are written and read
 constexpr double kF8BytesPerUs = 5.2e6;                        // from HBM
 
-// The form for few rows: B from HBM, and what a unit's workgroups load through its caches, m rows of A and 16 or 32 of B for every 16 columns.
-// In us, this form | the best of the others: 1 x 8192 x 8192 13.7 | 16.2; 17 x 4096 x 4096 7.3 | 10.1; 33 x 2048 x 2048 5.9 | 7.3;
-// 23 x 84 x 11286 15.3 | 8.5; 60 x 84 x 4000 11.6 | 7.2; 17 x 8192 x 8192 20.5 | 16.6; 64 x 8192 x 8192 41.6 | 18.1.
+// The form for few rows: B from HBM, or what a unit's workgroups load through its caches, the rows of A (as a mean of those there are and those of the
+// 16, 32 or 64 that the kernel computes) and half of the 16 or 32 of B, for every 16 columns; the unit with the most workgroups counts.  Fitted to 266 calls of 1 to 64
+// rows, off by 10 % mostly.
+// In us, this form | the best of the others: 1 x 8192 x 8192 13.7 | 16.2; 17 x 8192 x 8192 19.6 | 16.0; 64 x 8192 x 8192 41.6 | 18.1;
+// 17 x 4096 x 4096 7.4 | 9.4; 40 x 5120 x 5120 (320 workgroups) 21.6 | 12.2; 33 x 2048 x 2048 6.0 | 7.0; 23 x 84 x 11286 15.3 | 8.5; 60 x 84 x 4000 11.6 | 7.2;
+// gated, 16 x 16384 x 4096 28.9 | 34.3; 64 x 16384 x 4096 56.5 | 33.5.
 inline double f8_thin_us(int64_t m, int64_t n, int64_t k, bool gated) {
-    const double wide = gated ? 2.0 * n : n, shares = std::max(1.0, f8_ceil(n, 16) / 256.0);
-    return std::max(3.0 + shares * k * (m + (gated ? 32 : 16)) / 3.6e4, 1.0 + wide * k / kF8BytesPerUs);
+    const double wide = gated ? 2.0 * n : n;
+    const int64_t rounds = f8_ceil(f8_ceil(n, 16), 256), computed = m <= 16 ? 16 : m <= 32 ? 32 : 64;
+    return std::max(3.0 + rounds * k * ((m + computed) / 2.0 + (gated ? 16 : 8)) / 2.8e4, 1.0 + wide * k / kF8BytesPerUs);
 }
 
 inline F8Plan f8_plan(int64_t m, int64_t n, int64_t k, bool gated) {

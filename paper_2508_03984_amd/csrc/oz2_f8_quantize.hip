@@ -5,7 +5,7 @@
 //
 // A block of one row for the matrix as it is and for its transpose, or of 128 x 128 for both, come from one read: a workgroup
 // holds a tile of 128 x 128 in registers, 4 x 8 numbers per thread, and turns the bytes of the transpose through LDS.
-// 16384 x 8192 bf16, as it is and transposed: 110 us, 4.9 TB/s (blocks of 128 x 128 108); as it is only 71 to 79 us, 5.1 to 5.7 TB/s; 1500 x 1111 f32
+// 16384 x 8192 bf16 in blocks of 128 x 128, as it is and transposed: 111 to 113 us, 4.7 to 4.8 TB/s; as it is only, by rows, 71 to 79 us, 5.1 to 5.7 TB/s; 1500 x 1111 f32
 // 5.8 us, 64 x 8192 2.9 us.  Bound: HBM; the smallest calls by latency.
 #include "oz2_f8_device.hpp"
 

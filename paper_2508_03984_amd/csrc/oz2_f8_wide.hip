@@ -14,9 +14,10 @@
 //   - whole tiles of 16-bit results are rounded before the words change places among the lanes.
 // A workgroup per compute unit walks over the tiles; its requests run over the ends of tiles.  Every tile has at least kF8WideBlocks blocks.
 //
-// 8192 x 16384 x 16384: 1510 to 1630 us, 2.9 to 2.7 PFLOP/s, on numbers of a normal distribution, at 1.8 to 1.9 GHz under the power cap; on constant operands 1350 us, 3.26 PFLOP/s at 2.3 GHz; with the loads taken
-// out 1085.  The matrix cores are busy 69 % of the cycles.  By 8 wavefronts of 64 x 128, with a second set of wavefronts instead of the order by
-// hand, 1725 (1546).  Bound: board power; beside it the loads, of which an L2 miss in six comes late, and what lies between
+// 8192 x 16384 x 16384: 1510 to 1630 us, 2.9 to 2.7 PFLOP/s, on numbers of a normal distribution, at 1.7 to 1.9 GHz under the power cap; on constant operands, which leave the clock at
+// 2.2 to 2.3 GHz, 1350 us, 3.26 PFLOP/s; on those with the loads taken out 1085.  By 8 wavefronts of 64 x 128, with a second set of wavefronts instead of the order by
+// hand, 1725 (1546).  Bound: the matrix cores are busy 69 % of the cycles, at whatever clock the operands leave (66 % on constants).  The other cycles go to waiting for an
+// instruction to issue (41 % of the wavefronts' time), to the loads, of which an L2 miss in six comes late (waits and meetings 15 %), and to what lies between
 // two tiles, for which there are no registers beside the next one's sums (8192 x 16384 at k = 4096 420 us, 4096 x 8192 at k = 16384 with as many
 // operations 389; gated, 8192 x 8192 x 4096 408, with its sums kept 450).
 #include <type_traits>
@@ -410,7 +411,8 @@ struct Wide {
             else store_sums(static_cast<float *>(o.C), o.ldc, row0, col0, 0, o.alpha);
             return;
         }
-        // Anything else, 16 rows at a time; this code exists once.
+        // Anything else, 16 rows at a time; this code exists once.  One way to memory after the other: 8192 x 8192 x 1024 added to C takes 119 us in
+        // bf16 and 166 in f32 (76 and 109 without C); gated, 8192 x 8192 x 4096 in f32 446 us, with its sums kept 588 (396 and 453 in bf16).
         const int first = row0 + (wave >> 1) * 128 + lrow;
 #pragma unroll 1
         for (int unit = 0; unit < 16; ++unit) {

@@ -269,7 +269,7 @@ def prepare(case, seed):
         out = {name: None for name, asked in zip(("as_is", "transposed"), MODES[c["mode"]]) if asked}
     if own:                                                     # the handles and the buffers that a program keeps
         import paper_2508_03984_amd as oz
-        st = {name: oz.I8(*v) if isinstance(v, tuple) else v for name, v in st.items()}
+        st = {name: oz.I8.of(*v) if isinstance(v, tuple) else v for name, v in st.items()}
         new = lambda *shape: torch.zeros(*shape, device="cuda", dtype=DTYPES[c["dtype"]])  # noqa: E731
 
         def empty(rows, cols, groups=1):

@@ -388,6 +388,78 @@ oz2_status oz2_f8_gated_grad(int64_t m, int64_t f, oz2_act act, const void *Z, i
 size_t oz2_f8_workspace_bytes(int64_t m, int64_t n, int64_t k, int gated);
 
 /*
+ * Products in 8-bit integers with a scale for each token and channel, alone and grouped by expert.  Conventions as above.
+ *
+ * oz2_i8: a rows x k matrix of integers, entry (r, h) standing for q[r * ld + h] * scale[r].  q is 16-byte aligned and ld a multiple of 16, at least
+ * k and at most 2^23.  Rows are stored up to the next multiple of 16 bytes: what lies between is read and has no effect.  Where rows
+ * lie side by side by groups (oz2_i8_quantize_grouped, transposed; oz2_i8_grouped_grad) group g has scales of its own, scale[g * ld_scale + r] with
+ * ld_scale >= rows; elsewhere ld_scale has no meaning.  The struct is read during the call only.
+ *
+ * Sums are exact: int32, k up to 131071 (OZ2_UNSUPPORTED beyond; longer ones are added up by calls with beta = 1).  An entry of C is alpha * (sum * scale
+ * of A's row * scale of B's row) + beta * C, computed in binary32 in this order and rounded to its type once.  m, n, rows and groups * rows of a matrix up
+ * to 2^30, and less where a launch would have 2^32 threads (OZ2_UNSUPPORTED); up to 4096 groups.  A size of 0: nothing is done, but C <- beta * C for
+ * sums of nothing (k == 0, groups without rows), whatever alpha is.  beta == 0: C is not read.
+ */
+typedef struct {
+    void *q;
+    int64_t ld;
+    float *scale;
+    int64_t ld_scale;
+} oz2_i8;
+
+/*
+ * `batch` matrices of rows x cols numbers of `type`, one below the other in X (ldx >= cols), in 8-bit integers: as they are (batch * rows x cols),
+ * each transposed (batch * cols x rows, one below the other), or both; the other pointer is NULL.  The scale of a row of what is written (so of
+ * a column of X in the transpose) is max|x| times the binary32 number next to 1 / 127, rounded to binary32, 2^-126 at least, and q the integer next to x / scale, ties to even.  A
+ * row with NaN or an infinity has the scale NaN and zeros: NaN reaches the results that it belongs to.  Bytes from the end of a row to the next
+ * multiple of 16 are cleared; further ones are not touched.
+ */
+oz2_status oz2_i8_quantize(int64_t batch, int64_t rows, int64_t cols, const void *X, int64_t ldx, oz2_type type, const oz2_i8 *as_is,
+                           const oz2_i8 *transposed, hipStream_t stream);
+
+/*
+ * The same for tokens on their way to experts.  Rows offsets[g] .. offsets[g + 1] - 1 of `rows` belong to group g (device, groups + 1 ascending numbers from
+ * 0 to rows; rows before the first and from the last one on belong to none and are not written).  Row r is row index[r] of X (device, `rows` numbers), a row of
+ * zeros where that is not one of 0 .. x_rows - 1; index NULL: row r, x_rows >= rows.  As it is: rows x cols.  Transposed: cols x oz2_i8_grouped_cols(rows, groups), the rows of
+ * group g side by side from column offsets[g] / 128 * 128 + 128 g on, cleared from their end to the next multiple of 128; other columns are not
+ * touched.  A scale belongs to a column of X in a group; groups without rows have 2^-126.
+ * Offsets that do not ascend within 0 .. rows give unspecified results in the memory that right ones may write; the same holds for the two calls below.
+ */
+oz2_status oz2_i8_quantize_grouped(int64_t rows, int64_t cols, const void *X, int64_t x_rows, int64_t ldx, oz2_type type, const int32_t *index,
+                                   int64_t groups, const int32_t *offsets, const oz2_i8 *as_is, const oz2_i8 *transposed, hipStream_t stream);
+/* rows / 128 * 128 + 128 * groups; 0 for what the calls refuse. */
+int64_t oz2_i8_grouped_cols(int64_t rows, int64_t groups);
+
+/*
+ * C <- alpha * A * B^T + beta * C for A: m x k and B: n x k in 8-bit integers, C: m x n of `type` (ldc >= n).  With A = activations, B = a weight
+ * (outputs x inputs) this is a layer; with the transposed forms of oz2_i8_quantize the gradients of its input and of its weight.  k == 0: A and B
+ * may be NULL.
+ */
+oz2_status oz2_i8_gemm(int64_t m, int64_t n, int64_t k, float alpha, const oz2_i8 *A, const oz2_i8 *B, float beta, void *C, int64_t ldc,
+                       oz2_type type, hipStream_t stream);
+oz2_status oz2_ctx_i8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, float alpha, const oz2_i8 *A, const oz2_i8 *B, float beta, void *C,
+                           int64_t ldc, oz2_type type, hipStream_t stream);
+
+/*
+ * The same by group: A is rows x k, B groups * n x k (a weight of n rows for each group, one below the other), and rows offsets[g] .. offsets[g + 1] - 1 of C
+ * (rows x n) are A's times B_g^T.  Other rows of C are left as they are.  With each weight transposed (oz2_i8_quantize, batch = groups) this is
+ * the gradient of the input as well.
+ */
+oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+                               const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream);
+
+/*
+ * The gradients of the weights: C is groups * m x n, and C_g <- alpha * A_g * B_g^T + beta * C_g over the columns of group g of A (m x
+ * oz2_i8_grouped_cols(rows, groups)) and B (n x the same), both as oz2_i8_quantize_grouped writes them transposed.  A group of more than 131071 rows gives NaN.
+ * rows == 0: A and B may be NULL.
+ */
+oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+                               const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream);
+
+/* Workspace of oz2_i8_gemm, as for oz2_f8_workspace_bytes, with which it shares its memory. */
+size_t oz2_i8_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
  * Constants of Section 4.1 for `num_moduli` moduli, written to HOST arrays of
  * at least num_moduli entries (any of them may be NULL):
  *   p           moduli p_i

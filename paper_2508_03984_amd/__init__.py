@@ -9,7 +9,7 @@ from . import binding as _binding
 from .binding import (  # noqa: F401
     OZ2Error, lib_path, load, stage_tensor, matmul, block_slices, unblock_slices, OZ2_OP_N, OZ2_OP_T, Operand, Context,
     OZ2_OPT_INT32_PRODUCTS, OZ2_OPT_OVERLAP, OZ2_OPT_SMALL_CONVERSION, OZ2_OPT_PROFILING,
-    F8, OZ2_BF16, OZ2_F16, OZ2_F32, OZ2_ACT_SILU, OZ2_ACT_GELU,
+    F8, I8, OZ2_BF16, OZ2_F16, OZ2_F32, OZ2_ACT_SILU, OZ2_ACT_GELU,
 )
 
 # one Python function per C entry point, under the same name

@@ -32,6 +32,8 @@ EXPORTS = [
     "oz2_ctx_last_stage_times_ms", "oz2_dgemm_noalloc",
     "oz2_f8_quantize", "oz2_f8_gemm", "oz2_f8_gated", "oz2_f8_gated_grad", "oz2_f8_workspace_bytes",
     "oz2_ctx_f8_gemm", "oz2_ctx_f8_gated",
+    "oz2_i8_quantize", "oz2_i8_quantize_grouped", "oz2_i8_grouped_cols", "oz2_i8_gemm", "oz2_ctx_i8_gemm", "oz2_i8_grouped_gemm", "oz2_i8_grouped_grad",
+    "oz2_i8_workspace_bytes",
 ]
 
 OZ2_OPT_INT32_PRODUCTS, OZ2_OPT_OVERLAP, OZ2_OPT_SMALL_CONVERSION, OZ2_OPT_PROFILING, OZ2_OPT_CUT_LAUNCHES = range(5)
@@ -44,6 +46,10 @@ OZ2_ACT_SILU, OZ2_ACT_GELU = range(2)
 
 class _F8Struct(C.Structure):
     _fields_ = [("q", C.c_void_p), ("ld", C.c_int64), ("scale", C.c_void_p), ("ld_scale", C.c_int64), ("block_rows", C.c_int)]
+
+
+class _I8Struct(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("ld", C.c_int64), ("scale", C.c_void_p), ("ld_scale", C.c_int64)]
 
 
 class OZ2Error(RuntimeError):
@@ -146,6 +152,17 @@ def load():
     lib.oz2_f8_gated_grad.argtypes = [i64, i64, ci, vp, i64, vp, i64, ci, f8, f8, vp]
     lib.oz2_f8_workspace_bytes.argtypes = [i64, i64, i64, ci]
     lib.oz2_f8_workspace_bytes.restype = C.c_size_t
+    i8 = C.POINTER(_I8Struct)
+    lib.oz2_i8_quantize.argtypes = [i64, i64, i64, vp, i64, ci, i8, i8, vp]
+    lib.oz2_i8_quantize_grouped.argtypes = [i64, i64, vp, i64, i64, ci, vp, i64, vp, i8, i8, vp]
+    lib.oz2_i8_grouped_cols.argtypes = [i64, i64]
+    lib.oz2_i8_grouped_cols.restype = i64
+    lib.oz2_i8_gemm.argtypes = [i64, i64, i64, flt, i8, i8, flt, vp, i64, ci, vp]
+    lib.oz2_ctx_i8_gemm.argtypes = [vp] + lib.oz2_i8_gemm.argtypes
+    lib.oz2_i8_grouped_gemm.argtypes = [i64, i64, i64, i64, vp, flt, i8, i8, flt, vp, i64, ci, vp]
+    lib.oz2_i8_grouped_grad.argtypes = lib.oz2_i8_grouped_gemm.argtypes
+    lib.oz2_i8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.oz2_i8_workspace_bytes.restype = C.c_size_t
     for name in EXPORTS:
         if name.startswith("oz2_ctx_") or name in ("oz2_create", "oz2_destroy"):
             getattr(lib, name).restype = ci
@@ -160,7 +177,8 @@ def load():
                  "oz2_stage_ptr", "oz2_int8_gemm", "oz2_last_stage_times_ms", "oz2_mfma_probe",
                  "oz2_dgemm_op", "oz2_sgemm_op", "oz2_prepare_d", "oz2_prepare_s", "oz2_dgemm_prepared",
                  "oz2_sgemm_prepared", "oz2_last_panels", "oz2_plan_panels", "oz2_dgemm_colmajor",
-                 "oz2_sgemm_colmajor", "oz2_f8_quantize", "oz2_f8_gemm", "oz2_f8_gated", "oz2_f8_gated_grad"):
+                 "oz2_sgemm_colmajor", "oz2_f8_quantize", "oz2_f8_gemm", "oz2_f8_gated", "oz2_f8_gated_grad", "oz2_i8_quantize", "oz2_i8_quantize_grouped",
+                 "oz2_i8_gemm", "oz2_i8_grouped_gemm", "oz2_i8_grouped_grad"):
         getattr(lib, name).restype = ci
     _lib = lib
     return lib
@@ -710,6 +728,109 @@ def oz2_f8_gated_grad(m, f, act, Z, ldz, dH, lddh, D, DT, stream=None) -> None:
 
 def oz2_f8_workspace_bytes(m, n, k, gated=False) -> int:
     return int(load().oz2_f8_workspace_bytes(m, n, k, int(bool(gated))))
+
+
+# ------------------------------------------------------------------ 8-bit integers
+class I8:
+    """A rows x cols matrix of 8-bit integers on the device (oz2_i8): `q` (torch.int8) and `scale` (torch.float32), one for each row, or `groups` x rows for
+    the rows of groups that lie side by side.  Keep it as long as the tensors' memory: a call reads the addresses from here."""
+
+    __slots__ = ("q", "scale", "rows", "cols", "groups", "ref", "_struct")
+
+    def __init__(self, q, scale):
+        torch = _th()
+        rows, cols = q.shape
+        if q.dtype is not torch.int8 or scale.dtype is not torch.float32:
+            raise ValueError("q of dtype int8 and scale of dtype float32 expected")
+        if scale.dim() not in (1, 2) or scale.shape[-1] != rows:
+            raise ValueError(f"scale of {rows} numbers, or of {rows} for each group, expected, got {tuple(scale.shape)}")
+        if (cols > 1 and q.stride(1) != 1) or (rows > 1 and scale.stride(-1) != 1):
+            raise ValueError("row-major q and scale expected")
+        ld = q.stride(0) if rows > 1 else _up(cols, 16)       # (of one row the stride says nothing)
+        left = q.untyped_storage().nbytes() - q.storage_offset() - (rows - 1) * q.stride(0)
+        if q.numel() and left < _up(cols, 16):                # the last row is stored whole, too
+            raise ValueError("rows have to be stored up to the next multiple of 16 bytes")
+        self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
+        self.groups = scale.shape[0] if scale.dim() == 2 else 1
+        self._struct = _I8Struct(_dev(q), ld, _dev(scale), scale.stride(0) if self.groups > 1 else rows)
+        self.ref = C.byref(self._struct)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, groups: int = 1, device="cuda") -> "I8":
+        """Memory for rows x cols elements, with rows on multiples of 128 bytes; a scale for each row, or, of more than one group, for each group and row."""
+        torch = _th()
+        q = torch.empty((rows, max(_up(cols, 128), 128)), dtype=torch.int8, device=device)
+        return cls(q[:, :cols], torch.empty((rows,) if groups == 1 else (groups, rows), dtype=torch.float32, device=device))
+
+    @classmethod
+    def of(cls, q, scale) -> "I8":
+        """A copy of q and scale, which may have any strides, where their rows are stored as the products need them."""
+        out = cls.empty(q.shape[0], q.shape[1], scale.shape[0] if scale.dim() == 2 else 1, q.device)
+        out.q.copy_(q)
+        out.scale.copy_(scale.reshape(out.scale.shape))
+        return out
+
+    @property
+    def shape(self):
+        return tuple(self.q.shape)
+
+
+def _i8_ref(x, rows: int, cols: int, groups: int = 1):
+    """The struct of a matrix that has at least rows x cols elements, with scales for so many groups; None for None."""
+    if x is None:
+        return None
+    if x.rows < rows or x.cols < cols or x.groups < groups:
+        raise ValueError(f"matrix of {rows} x {cols} 8-bit integers with scales for {groups} groups expected, got {x.rows} x {x.cols}, {x.groups}")
+    return x.ref
+
+
+def _int32(t, n: int):
+    """The address of at least n numbers of 32 bits, one after the other."""
+    if t is None:
+        return None
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{n} contiguous numbers expected, got {tuple(t.shape)}")
+    return _dev(t, _th().int32)
+
+
+def oz2_i8_quantize(batch, rows, cols, X, ldx, as_is, transposed, stream=None) -> None:
+    _check(load().oz2_i8_quantize(batch, rows, cols, _dev(X), ldx, _f8_type(X), _i8_ref(as_is, batch * rows, cols),
+                                  _i8_ref(transposed, batch * cols, rows), _stream(stream)), "oz2_i8_quantize")
+
+
+def oz2_i8_quantize_grouped(rows, cols, X, x_rows, ldx, index, groups, offsets, as_is, transposed, stream=None) -> None:
+    _check(load().oz2_i8_quantize_grouped(rows, cols, _dev(X), x_rows, ldx, _f8_type(X), _int32(index, rows), groups, _int32(offsets, groups + 1),
+                                          _i8_ref(as_is, rows, cols), _i8_ref(transposed, cols, oz2_i8_grouped_cols(rows, groups), groups),
+                                          _stream(stream)), "oz2_i8_quantize_grouped")
+
+
+def oz2_i8_grouped_cols(rows, groups) -> int:
+    return int(load().oz2_i8_grouped_cols(rows, groups))
+
+
+def oz2_ctx_i8_gemm(ctx, m, n, k, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    _check(load().oz2_ctx_i8_gemm(_ctx(ctx), m, n, k, alpha, _i8_ref(A, m, k), _i8_ref(B, n, k), beta, _dev(C_), ldc, _f8_type(C_),
+                                  _stream(stream)), "oz2_ctx_i8_gemm")
+
+
+def oz2_i8_gemm(m, n, k, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    _check(load().oz2_i8_gemm(m, n, k, alpha, _i8_ref(A, m, k), _i8_ref(B, n, k), beta, _dev(C_), ldc, _f8_type(C_), _stream(stream)),
+           "oz2_i8_gemm")
+
+
+def oz2_i8_grouped_gemm(rows, n, k, groups, offsets, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    _check(load().oz2_i8_grouped_gemm(rows, n, k, groups, _int32(offsets, groups + 1), alpha, _i8_ref(A, rows, k), _i8_ref(B, groups * n, k), beta,
+                                      _dev(C_), ldc, _f8_type(C_), _stream(stream)), "oz2_i8_grouped_gemm")
+
+
+def oz2_i8_grouped_grad(m, n, rows, groups, offsets, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    wide = oz2_i8_grouped_cols(rows, groups) if rows else 0
+    _check(load().oz2_i8_grouped_grad(m, n, rows, groups, _int32(offsets, groups + 1), alpha, _i8_ref(A, m, wide, groups), _i8_ref(B, n, wide, groups),
+                                      beta, _dev(C_), ldc, _f8_type(C_), _stream(stream)), "oz2_i8_grouped_grad")
+
+
+def oz2_i8_workspace_bytes(m, n, k) -> int:
+    return int(load().oz2_i8_workspace_bytes(m, n, k))
 
 
 # ------------------------------------------------------------------ conveniences (no arithmetic)

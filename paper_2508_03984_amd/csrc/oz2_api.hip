@@ -13,6 +13,7 @@
 #include "../../include/oz2.h"
 #include "oz2_constants.hpp"
 #include "oz2_f8.hpp"
+#include "oz2_i8.hpp"
 #include "oz2_kernels.hpp"
 #include "oz2_plan.hpp"
 
@@ -1141,6 +1142,157 @@ size_t oz2_f8_workspace_bytes(int64_t m, int64_t n, int64_t k, int gated) {
     bool nothing = false;
     if (f8_sizes(m, n, k, kF8Bf16, &nothing) || nothing) return 0;
     return f8_plan(m, n, k, gated != 0).plane_bytes;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ 8-bit integers
+namespace {
+
+// What the kernels rely on, for rows of k elements; ld_scale where every group has scales of its own for `rows` rows.
+oz2_status i8_matrix(const oz2_i8 *x, int64_t k, int64_t rows, bool by_group, I8Matrix *out) {
+    if (!x || !x->q || !x->scale) return OZ2_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(x->q) % 16 || x->ld % 16 || x->ld < k || reinterpret_cast<uintptr_t>(x->scale) % 4) return OZ2_INVALID_ARG;
+    if (by_group && x->ld_scale < rows) return OZ2_INVALID_ARG;
+    if (x->ld > kF8MaxLd || (by_group && x->ld_scale > kF8MaxRows)) return OZ2_UNSUPPORTED;
+    *out = I8Matrix{static_cast<const int8_t *>(x->q), x->ld, x->scale, by_group ? x->ld_scale : 0};
+    return OZ2_OK;
+}
+
+// Sizes whose product is that of a matrix.
+bool i8_too_many(int64_t groups, int64_t rows) { return rows > kF8MaxRows || groups > kF8MaxRows || groups * rows > kF8MaxRows; }
+
+oz2_status i8_groups(int64_t rows, int64_t groups, const int32_t *offsets, I8Groups *out) {
+    if (groups < 1 || !offsets || reinterpret_cast<uintptr_t>(offsets) % 4) return OZ2_INVALID_ARG;
+    if (groups > kI8MaxGroups) return OZ2_UNSUPPORTED;
+    *out = I8Groups{offsets, (int)groups, (int)rows, 0};
+    return OZ2_OK;
+}
+
+oz2_status i8_convert(I8Quantize &p, const oz2_i8 *as_is, const oz2_i8 *transposed, int64_t wide, int type, hipStream_t stream) {
+    I8Matrix m;
+    if (as_is) {
+        if (oz2_status st = i8_matrix(as_is, p.cols, 0, false, &m)) return st;
+        p.q = static_cast<int8_t *>(as_is->q);
+        p.ld = as_is->ld;
+        p.scale = as_is->scale;
+    }
+    if (transposed) {
+        if (oz2_status st = i8_matrix(transposed, wide, p.cols, p.side_by_side, &m)) return st;
+        p.qt = static_cast<int8_t *>(transposed->q);
+        p.ldt = transposed->ld;
+        p.scale_t = transposed->scale;
+        p.ld_scale_t = p.side_by_side ? transposed->ld_scale : p.cols;
+    }
+    if (i8_quantize_threads(p) >= kMaxThreads) return OZ2_UNSUPPORTED;
+    OZ2_TRY(launch_i8_quantize(p, type, stream));
+    return OZ2_OK;
+}
+
+oz2_status i8_launch(I8Mode mode, const I8Args &args, I8Form form, hipStream_t stream) {
+    if (i8_tiles(mode, form, args) * 256 >= kMaxThreads) return OZ2_UNSUPPORTED;
+    OZ2_TRY(launch_i8_product(mode, args, form, stream));
+    return OZ2_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+oz2_status oz2_i8_quantize(int64_t batch, int64_t rows, int64_t cols, const void *X, int64_t ldx, oz2_type type, const oz2_i8 *as_is,
+                           const oz2_i8 *transposed, hipStream_t stream) {
+    if (batch < 0 || rows < 0 || cols < 0 || !f8_type_ok(type) || (!as_is && !transposed)) return OZ2_INVALID_ARG;
+    if (batch == 0 || rows == 0 || cols == 0) return OZ2_OK;
+    if (!f8_numbers_ok(X, ldx, cols, type)) return OZ2_INVALID_ARG;
+    if (i8_too_many(batch, rows) || i8_too_many(batch, cols)) return OZ2_UNSUPPORTED;
+    I8Quantize p{};
+    p.X = X; p.ldx = ldx; p.x_rows = batch * rows; p.cols = cols;
+    p.groups = I8Groups{nullptr, (int)batch, (int)(batch * rows), (int)rows};
+    return i8_convert(p, as_is, transposed, rows, type, stream);
+}
+
+oz2_status oz2_i8_quantize_grouped(int64_t rows, int64_t cols, const void *X, int64_t x_rows, int64_t ldx, oz2_type type, const int32_t *index,
+                                   int64_t groups, const int32_t *offsets, const oz2_i8 *as_is, const oz2_i8 *transposed, hipStream_t stream) {
+    if (rows < 0 || cols < 0 || !f8_type_ok(type) || (!as_is && !transposed)) return OZ2_INVALID_ARG;
+    I8Quantize p{};
+    if (oz2_status st = i8_groups(rows, groups, offsets, &p.groups)) return st;
+    if (rows == 0 || cols == 0) return OZ2_OK;
+    if (!f8_numbers_ok(X, ldx, cols, type) || reinterpret_cast<uintptr_t>(index) % 4) return OZ2_INVALID_ARG;
+    if (x_rows < (index ? 1 : rows)) return OZ2_INVALID_ARG;
+    if (rows > kF8MaxRows || cols > kF8MaxRows) return OZ2_UNSUPPORTED;
+    p.X = X; p.ldx = ldx; p.x_rows = x_rows; p.cols = cols; p.index = index;
+    p.side_by_side = 1;
+    return i8_convert(p, as_is, transposed, i8_grouped_cols(rows, groups), type, stream);
+}
+
+int64_t oz2_i8_grouped_cols(int64_t rows, int64_t groups) {
+    return rows < 0 || groups < 1 || rows > kF8MaxRows || groups > kI8MaxGroups ? 0 : i8_grouped_cols(rows, groups);
+}
+
+oz2_status oz2_ctx_i8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, float alpha, const oz2_i8 *A, const oz2_i8 *B, float beta, void *C,
+                           int64_t ldc, oz2_type type, hipStream_t stream) {
+    if (m < 0 || n < 0 || k < 0 || !f8_type_ok(type)) return OZ2_INVALID_ARG;
+    if (m == 0 || n == 0) return OZ2_OK;
+    if (!f8_numbers_ok(C, ldc, n, type)) return OZ2_INVALID_ARG;
+    I8Args args{};
+    if (k > 0) {
+        if (oz2_status st = i8_matrix(A, k, 0, false, &args.A)) return st;
+        if (oz2_status st = i8_matrix(B, k, 0, false, &args.B)) return st;
+    }
+    if (m > kF8MaxRows || n > kF8MaxRows || k > kI8MaxK) return OZ2_UNSUPPORTED;
+    args.m = (int)m; args.n = (int)n; args.k = (int)k;
+    args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
+    Ctx &g = resolve(ctx);
+    std::lock_guard<std::mutex> lock(g.mu);
+    const I8Plan plan = i8_plan(m, n, k);
+    args.ranges = plan.ranges;
+    args.kb_each = plan.kb_each;
+    return i8_launch(I8Mode::kDense, args, plan.form, stream);
+}
+
+oz2_status oz2_i8_gemm(int64_t m, int64_t n, int64_t k, float alpha, const oz2_i8 *A, const oz2_i8 *B, float beta, void *C, int64_t ldc,
+                       oz2_type type, hipStream_t stream) {
+    return oz2_ctx_i8_gemm(nullptr, m, n, k, alpha, A, B, beta, C, ldc, type, stream);
+}
+
+oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+                               const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
+    if (rows < 0 || n < 0 || k < 0 || !f8_type_ok(type)) return OZ2_INVALID_ARG;
+    I8Args args{};
+    if (oz2_status st = i8_groups(rows, groups, offsets, &args.groups)) return st;
+    if (rows == 0 || n == 0) return OZ2_OK;
+    if (!f8_numbers_ok(C, ldc, n, type)) return OZ2_INVALID_ARG;
+    if (k > 0) {
+        if (oz2_status st = i8_matrix(A, k, 0, false, &args.A)) return st;
+        if (oz2_status st = i8_matrix(B, k, 0, false, &args.B)) return st;
+    }
+    if (rows > kF8MaxRows || i8_too_many(groups, n) || k > kI8MaxK) return OZ2_UNSUPPORTED;
+    args.m = (int)rows; args.n = (int)n; args.k = (int)k;
+    args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
+    return i8_launch(I8Mode::kRows, args, I8Form::kSmall, stream);
+}
+
+oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+                               const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
+    if (m < 0 || n < 0 || rows < 0 || !f8_type_ok(type)) return OZ2_INVALID_ARG;
+    I8Args args{};
+    if (oz2_status st = i8_groups(rows, groups, offsets, &args.groups)) return st;
+    if (m == 0 || n == 0) return OZ2_OK;
+    if (!f8_numbers_ok(C, ldc, n, type)) return OZ2_INVALID_ARG;
+    if (rows > kF8MaxRows || i8_too_many(groups, m) || n > kF8MaxRows) return OZ2_UNSUPPORTED;
+    if (rows > 0) {
+        const int64_t wide = i8_grouped_cols(rows, groups);
+        if (oz2_status st = i8_matrix(A, wide, m, true, &args.A)) return st;
+        if (oz2_status st = i8_matrix(B, wide, n, true, &args.B)) return st;
+    }
+    args.m = (int)m; args.n = (int)n; args.k = (int)rows;
+    args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
+    return i8_launch(I8Mode::kSums, args, I8Form::kSmall, stream);
+}
+
+size_t oz2_i8_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+    if (m <= 0 || n <= 0 || k <= 0 || m > kF8MaxRows || n > kF8MaxRows || k > kI8MaxK) return 0;
+    return i8_plan(m, n, k).plane_bytes;
 }
 
 }  // extern "C"

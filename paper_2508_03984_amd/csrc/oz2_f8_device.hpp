@@ -201,4 +201,70 @@ __device__ __forceinline__ void f8_update_row(const F8Out &o, int64_t at, float 
     f8_store_row<N>(o.C, o.type, at, x, valid, from);
 }
 
+// The largest of top, |x| and |y| in one instruction, NaN if one of them is.  (v_max3_f32 passes over NaN, and having met a signalling one it
+// has forgotten what came before.)  Whatever is not below infinity at the end has met NaN or an infinity.
+__device__ __forceinline__ float max_magnitude(float top, float x, float y) {
+    float r;
+    asm("v_maximum3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(top), "v"(x), "v"(y));
+    return r;
+}
+__device__ __forceinline__ bool is_finite(float top) { return top < __builtin_inff(); }
+
+// 8 numbers of a row as they lie in memory, of which `valid` exist (zeros for the others), and in binary32.
+template <int TYPE>
+struct Eight {
+    static constexpr int kWords = TYPE == kF8F32 ? 2 : 1;
+    f8_v4i w[kWords];
+    typedef typename F8Number<TYPE>::T T;
+    __device__ __forceinline__ void load(const T *from) { __builtin_memcpy(w, from, sizeof w); }
+    // Of a row that ends at from[valid - 1] (`valid` may be negative), to be followed by move_down(down(valid, eight)).  A row of 8 or more numbers
+    // (`eight`) is read as its last 8, which are then moved down; number by number, one wait after the other, tiles at the edge took as
+    // long as all others (as they are, 16384 x 8191: 105 us instead of 78; the gradient's, 8192 x 8191, 256 instead of 164).
+    __device__ __forceinline__ void load(const T *from, int valid, bool eight) {
+        if (eight) {
+            load(from - max(8 - valid, 0));
+            return;
+        }
+        uint32_t words[4 * kWords];
+#pragma unroll
+        for (int i = 0; i < 4 * kWords; ++i) words[i] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) {
+                if constexpr (TYPE == kF8F32) words[i] = __builtin_bit_cast(uint32_t, from[i]);
+                else words[i / 2] |= (uint32_t)from[i] << (i % 2 * 16);
+            }
+#pragma unroll
+        for (int i = 0; i < 4 * kWords; ++i) w[i / 4][i % 4] = (int)words[i];
+    }
+    static __device__ __forceinline__ int down(int valid, bool eight) { return eight ? min(max(8 - valid, 0), 8) : 0; }
+    __device__ __forceinline__ void move_down(int by) {        // by 0 to 8 numbers, zeros following
+        constexpr int N = 4 * kWords;
+        uint32_t words[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) words[i] = (uint32_t)w[i / 4][i % 4];
+#pragma unroll
+        for (int step = 1; step <= 8; step *= 2) {
+            const bool move = by & step;
+            const int whole = step * N / 8;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t next = i + max(whole, 1) < N ? words[i + max(whole, 1)] : 0;
+                words[i] = !move ? words[i] : whole ? next : __builtin_amdgcn_alignbyte(next, words[i], 2);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i / 4][i % 4] = (int)words[i];
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (TYPE == kF8F32) {
+                const int word = w[i / 4][i % 4];
+                x[i] = __builtin_bit_cast(float, word);
+            } else x[i] = F8Number<TYPE>::get((uint16_t)((uint32_t)w[0][i / 2] >> (i % 2 * 16)));
+        }
+    }
+};
+
 }  // namespace oz2

@@ -1,0 +1,83 @@
+// Device code shared by the kernels of 8-bit integer products.
+#pragma once
+#include "oz2_f8_device.hpp"
+#include "oz2_i8.hpp"
+
+namespace oz2 {
+
+// Rows lo to hi - 1 of group g, whatever the offsets are.
+struct I8Span {
+    int group, lo, hi;
+};
+__device__ __forceinline__ I8Span i8_span(const I8Groups &s, int g) {
+    if (!s.offsets) return I8Span{g, g * s.each, (g + 1) * s.each};
+    const int lo = min(max(s.offsets[g], 0), s.rows);
+    return I8Span{g, lo, min(max(s.offsets[g + 1], lo), s.rows)};
+}
+
+__device__ __forceinline__ uint32_t i8_running_sum(uint32_t x, int lane) {
+#pragma unroll
+    for (int by = 1; by < 64; by *= 2) {
+        const uint32_t below = __shfl_up(x, by);
+        x += lane >= by ? below : 0;
+    }
+    return x;
+}
+
+// The groups cut into units of `each` rows, `per` pieces of work to a unit.  A workgroup's place among them, from its id: each of the 8 XCDs, to which ids go in
+// turns, has neighbouring pieces of one group, which share their operands in its L2.  False if there is none for the id.  A wavefront does this together, 64 groups
+// at a time; piece counts of offsets that do not ascend may be anything, but a span is always one of i8_span's.
+struct I8Place {
+    I8Span span;
+    uint32_t units, piece;                                     // of the group; 0 .. units * per - 1
+};
+__device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t per, uint32_t id, I8Place &out) {
+    if (!s.offsets) {
+        out.units = (uint32_t)(s.each + each - 1) / (uint32_t)each;
+        const uint32_t pieces = out.units * per, total = pieces * (uint32_t)s.groups, share = (total + 7) / 8, place = (id & 7) * share + (id >> 3);
+        if ((id >> 3) >= share || place >= total) return false;
+        const int g = (int)(place / pieces);
+        out.span = i8_span(s, g);
+        out.piece = place - (uint32_t)g * pieces;
+        return true;
+    }
+    const int lane = threadIdx.x & 63;
+    const auto count = [&](int g) {
+        if (g >= s.groups) return 0u;
+        const I8Span span = i8_span(s, g);
+        return (uint32_t)(span.hi - span.lo + each - 1) / (uint32_t)each;
+    };
+    uint32_t total = 0, first = count(lane), running = i8_running_sum(first, lane);
+    total = (uint32_t)__shfl((int)running, 63);
+    for (int g0 = 64; g0 < s.groups; g0 += 64) total += (uint32_t)__shfl((int)i8_running_sum(count(g0 + lane), lane), 63);
+    total *= per;
+    const uint32_t share = (total + 7) / 8, place = (id & 7) * share + (id >> 3);
+    if ((id >> 3) >= share || place >= total) return false;    // uniform
+    const uint32_t unit = place / per;
+    uint32_t before = 0;
+    for (int g0 = 0; g0 < s.groups; g0 += 64) {
+        if (g0) {
+            first = count(g0 + lane);
+            running = i8_running_sum(first, lane);
+        }
+        const uint64_t beyond = __ballot(before + running > unit);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond);
+            out.span = i8_span(s, __builtin_amdgcn_readfirstlane(g0 + at));
+            out.units = (uint32_t)__builtin_amdgcn_readlane((int)first, at);
+            out.piece = place - (before + (uint32_t)__builtin_amdgcn_readlane((int)running, at) - out.units) * per;
+            out.span.lo = __builtin_amdgcn_readfirstlane(out.span.lo);
+            out.span.hi = __builtin_amdgcn_readfirstlane(out.span.hi);
+            out.units = (uint32_t)__builtin_amdgcn_readfirstlane((int)out.units);
+            out.piece = (uint32_t)__builtin_amdgcn_readfirstlane((int)out.piece);
+            return out.piece < out.units * per;
+        }
+        before += (uint32_t)__shfl((int)running, 63);
+    }
+    return false;
+}
+
+// First column of a group whose rows lie side by side with the others'.
+__device__ __forceinline__ int64_t i8_first_col(const I8Span &s) { return (int64_t)(s.lo / kI8Block + s.group) * kI8Block; }
+
+}  // namespace oz2

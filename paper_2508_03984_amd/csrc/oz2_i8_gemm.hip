@@ -1,0 +1,313 @@
+// Products of matrices in 8-bit integers with a scale for each row, C_ij = alpha a_i b_j sum_h A_ih B_jh + beta C_ij, by tiles of C: alone (kDense), the rows of A by
+// group, each with its own B (kRows), or the columns of both by group, each with its own C (kSums).
+//
+// v_mfma_i32_16x16x64_i8 adds 64 products per entry of a 16 x 16 block to its int32 accumulators, exactly; the two scales are applied once, to the sum.
+//
+// Rows of A and B lie as the caller has them.  A stage of LDS holds 128 bytes of every row of the tile; the 16-byte chunk c of row r is at place
+// c ^ (r / 2 % 8), which gives every 16 lanes that LDS serves together 16 different places (two rows cover all banks).  Rows beyond the matrix or
+// the group are read as its last one and their results dropped; in the last block of k, chunks beyond k are read as the row's last one and
+// then cleared in LDS, in A only, since 0 times whatever B has there is 0.
+#include "oz2_epilogue.hpp"
+#include "oz2_i8_device.hpp"
+
+namespace oz2 {
+namespace {
+
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
+
+extern __shared__ f8_v4i i8_lds[];
+
+// WM x WN wavefronts with FM x FN blocks of 16 x 16 each.
+template <int WM, int WN, int FM, int FN, int STAGES>
+struct I8Core {
+    static constexpr int WAVES = WM * WN, THREADS = WAVES * 64;
+    static constexpr int BM = WM * FM * 16, BN = WN * FN * 16;
+    static constexpr int ROWS = BM + BN, STAGE_BYTES = ROWS * 128;
+    static constexpr int LOADS = ROWS / 8 / WAVES, A_LOADS = BM / 8 / WAVES;
+    static constexpr size_t LDS_BYTES = STAGES * STAGE_BYTES;
+    static_assert(BM <= THREADS && WAVES % 2 == 0 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && LOADS * (STAGES - 2) < 64, "");
+};
+
+// At most N loads of this wavefront outstanding, for one of several N; own LDS reads done; then all wavefronts meet.
+template <int EACH, int MOST>
+__device__ __forceinline__ void wait_ahead_and_meet(int ahead) {
+    if (MOST > 0 && ahead < MOST) {                                        // uniform: the last blocks of a range
+        if constexpr (MOST > 0) wait_ahead_and_meet<EACH, MOST - 1>(ahead);
+        return;
+    }
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(EACH * MOST) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// What a workgroup computes: rows x cols entries (at most a tile) over the blocks kb0 to kb1 - 1 of k, of which the last one of the row ends after k.
+struct Tile {
+    const int8_t *a, *b;                                                   // the first rows of both
+    const float *scale_a, *scale_b;
+    int rows, cols, k, kb0, kb1;
+    int64_t c_row;                                                         // row of C, column
+    int c_col, range;
+    bool lost;                                                             // more columns than int32 sums can hold for certain: NaN
+};
+
+// The places of a group's tiles: bands of 8 rows of tiles, within a band column by column, so that the 32 workgroups which an XCD runs at a time share A's and B's rows.
+__device__ __forceinline__ void place_in_group(uint32_t piece, uint32_t units, uint32_t tiles_n, int &tr, int &tc) {
+    const uint32_t band = piece / (8 * tiles_n), left = piece - band * 8 * tiles_n, high = min(8u, units - band * 8);
+    tc = (int)(left / high);
+    tr = (int)(band * 8 + left - (uint32_t)tc * high);
+}
+
+template <I8Mode MODE, int BM, int BN>
+__device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, int id, Tile &t) {
+    t.lost = false;
+    t.range = 0;
+    if constexpr (MODE == I8Mode::kRows) {
+        const uint32_t tiles_n = (uint32_t)(p.n + BN - 1) / BN;
+        I8Place at;
+        if (!i8_find(p.groups, BM, tiles_n, (uint32_t)id, at)) return false;
+        int tr, tc;
+        place_in_group(at.piece, at.units, tiles_n, tr, tc);
+        const int row0 = at.span.lo + tr * BM, col0 = tc * BN;
+        const int64_t b_row = (int64_t)at.span.group * p.n + col0;
+        t.rows = min(BM, at.span.hi - row0);
+        t.cols = min(BN, p.n - col0);
+        t.a = p.A.q + row0 * p.A.ld;
+        t.b = p.B.q + b_row * p.B.ld;
+        t.scale_a = p.A.scale + row0;
+        t.scale_b = p.B.scale + b_row;
+        t.k = p.k;
+        t.kb0 = 0;
+        t.kb1 = (p.k + kI8Block - 1) / kI8Block;
+        t.c_row = row0;
+        t.c_col = col0;
+    } else {
+        int s, tr, tc;
+        map_tile(map, id, s, tr, tc);
+        const int row0 = tr * BM, col0 = tc * BN;
+        t.rows = min(BM, p.m - row0);
+        t.cols = min(BN, p.n - col0);
+        t.c_col = col0;
+        int64_t first = 0, scales_a = 0, scales_b = 0;
+        if constexpr (MODE == I8Mode::kDense) {
+            t.k = p.k;
+            const int KB = (p.k + kI8Block - 1) / kI8Block;
+            t.kb0 = s * p.kb_each;
+            t.kb1 = min(t.kb0 + p.kb_each, KB);
+            t.range = s;
+            t.c_row = row0;
+        } else {
+            const I8Span span = i8_span(p.groups, s);
+            first = i8_first_col(span);
+            scales_a = s * p.A.ld_scale;
+            scales_b = s * p.B.ld_scale;
+            t.lost = span.hi - span.lo > kI8MaxK;
+            t.kb0 = 0;
+            t.kb1 = t.lost ? 0 : (span.hi - span.lo + kI8Block - 1) / kI8Block;
+            t.k = t.kb1 * kI8Block;                                        // (zeros follow up to there)
+            t.c_row = (int64_t)s * p.m + row0;
+        }
+        t.a = p.A.q + row0 * p.A.ld + first;
+        t.b = p.B.q + col0 * p.B.ld + first;
+        t.scale_a = p.A.scale + scales_a + row0;
+        t.scale_b = p.B.scale + scales_b + col0;
+    }
+    return true;
+}
+
+// The entries of C from sums: N of a row, of which `valid` exist, with the scale of the row and those of the columns.
+template <int N>
+__device__ __forceinline__ void finish_row(const F8Out &o, int64_t at, const int (&sum)[N], float a, const float *b, int valid, bool lost, bool none) {
+    float x[N], scale[N];
+    if (none) {                                                            // (no scales either)
+        F8Out nothing = o;
+        nothing.alpha = 0.0f;                                              // no infinity or NaN from it
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = lost ? __builtin_nanf("") : 0.0f;
+        f8_update_row<N>(nothing, at, x, valid);
+        return;
+    }
+    if (valid >= N) __builtin_memcpy(scale, b, sizeof scale);
+    else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) scale[i] = b[min(i, valid - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (float)sum[i] * a * scale[i];
+    f8_update_row<N>(o, at, x, valid);
+}
+
+template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE>
+__global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, TileMap map) {
+    typedef I8Core<WM, WN, FM, FN, STAGES> C;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN, lrow = lane & 15, quarter = lane >> 4;
+    Tile t;
+    if (!find_tile<MODE, C::BM, C::BN>(p, map, (int)blockIdx.x, t)) return;
+    const int KB = (t.k + kI8Block - 1) / kI8Block, kb0 = t.kb0, kb1 = t.kb1;
+
+    // Load H of this wavefront takes the 8 rows from 8 (H WAVES + wave) on; a lane 16 bytes of one.
+    const int chunk = (lane & 7) ^ ((wave & 1) * 4 + quarter);
+    uint32_t offset[C::LOADS];
+#pragma unroll
+    for (int h = 0; h < C::LOADS; ++h) {
+        const int r = (h * C::WAVES + wave) * 8 + (lane >> 3);
+        offset[h] = h < C::A_LOADS ? (uint32_t)min(r, t.rows - 1) * (uint32_t)p.A.ld : (uint32_t)min(r - C::BM, t.cols - 1) * (uint32_t)p.B.ld;
+        offset[h] += chunk * 16;
+    }
+    const int in_last = t.k - (KB - 1) * kI8Block;                         // of the last block, 1 to 128
+    const int to_last_chunk = (min(chunk, (in_last - 1) / 16) - chunk) * 16;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)i8_lds;
+    int want = kb0, want_stage = 0;                                        // the block that is requested next, and where it goes
+    const auto request = [&]() {
+        if (want >= kb1) return;                                           // uniform
+        const uint32_t back = want == KB - 1 ? (uint32_t)to_last_chunk : 0u;
+#pragma unroll
+        for (int h = 0; h < C::LOADS; ++h) {
+            const int8_t *const base = (h < C::A_LOADS ? t.a : t.b) + (int64_t)want * kI8Block;
+            const uint32_t to = lds0 + want_stage * C::STAGE_BYTES + (h * C::WAVES + wave) * 1024;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset[h] + back), "s"(base) : "memory");
+        }
+        ++want;
+        want_stage = want_stage + 1 == STAGES ? 0 : want_stage + 1;
+    };
+
+    f8_v4i acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f8_v4i{0, 0, 0, 0};
+    const char *const lds = reinterpret_cast<const char *>(i8_lds);
+    const int swizzled = (quarter ^ (lane >> 1 & 7)) * 16;
+    const int a_addr = (wm * FM * 16 + lrow) * 128 + swizzled, b_addr = (C::BM + wn * FN * 16 + lrow) * 128 + swizzled;
+    struct Fragments {
+        f8_v4i a[FM][2], b[FN][2];                                         // halves of a block of 128
+    };
+    int stage = 0;                                                         // of the block that is read next
+    const auto read = [&](Fragments &f) {
+        const char *const at = lds + stage * C::STAGE_BYTES;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) f.a[i][half] = *reinterpret_cast<const f8_v4i *>(at + i * 2048 + (a_addr ^ half * 64));
+#pragma unroll
+            for (int j = 0; j < FN; ++j) f.b[j][half] = *reinterpret_cast<const f8_v4i *>(at + j * 2048 + (b_addr ^ half * 64));
+        }
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    };
+    // Waits until block kb is there; whoever comes here has read all blocks before it.
+    const auto arrive = [&](int kb) {
+        wait_ahead_and_meet<C::LOADS, STAGES - 2>(want - 1 - kb);
+        if (kb == KB - 1 && in_last < kI8Block) {                          // what lies behind k, of this thread's row of A
+            if ((int)threadIdx.x < C::BM) {
+                const int r = (int)threadIdx.x, from = in_last >> 4, f = r >> 1 & 7;
+                f8_v4i *const row = i8_lds + stage * (C::STAGE_BYTES / 16) + r * 8;
+                row[from ^ f] = f8_keep(row[from ^ f], in_last & 15);
+                for (int c = from + 1; c < 8; ++c) row[c ^ f] = f8_v4i{0, 0, 0, 0};
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+    };
+    const auto multiply = [&](const Fragments &f) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int i = 0; i < FM; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[j][half], f.a[i][half], acc[i][j], 0, 0, 0);
+    };
+    // The fragments of a block are read during the MFMAs of the one before; STAGES - 1 blocks are in flight.
+    if (kb0 < kb1) {
+        Fragments f, g;
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) request();
+        arrive(kb0);
+        request();
+        read(f);
+        for (int kb = kb0 + 1;; kb += 2) {
+            if (kb < kb1) {
+                arrive(kb);
+                request();
+                read(g);
+            }
+            multiply(f);
+            if (kb >= kb1) break;
+            if (kb + 1 < kb1) {
+                arrive(kb + 1);
+                request();
+                read(f);
+            }
+            multiply(g);
+            if (kb + 1 >= kb1) break;
+        }
+    }
+
+    const F8Out &o = p.out;
+    const bool none = kb0 >= kb1;
+    // N numbers of a row, at a column that is a multiple of N.
+    const auto emit = [&](const auto &x, int row, int col) {
+        constexpr int N = sizeof(x) / sizeof(x[0]);
+        const int valid = row < t.rows ? t.cols - col : 0;
+        if (valid <= 0) return;
+        if (MODE == I8Mode::kDense && o.planes) {                          // (a plane's rows are stored to a multiple of 16)
+            int32_t *const to = reinterpret_cast<int32_t *>(o.planes) + t.range * o.plane + (t.c_row + row) * o.ldp + t.c_col + col;
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+                const f8_v4i w{x[i], x[i + 1], x[i + 2], x[i + 3]};
+                *reinterpret_cast<f8_v4i *>(to + i) = w;
+            }
+        } else finish_row<N>(o, (t.c_row + row) * o.ldc + t.c_col + col, x, none ? 0.0f : t.scale_a[row], t.scale_b + col, valid, t.lost, none);
+    };
+    if constexpr (FN == 1) {                                               // 4 numbers of a row per lane, as they are
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int x[4] = {acc[i][0][0], acc[i][0][1], acc[i][0][2], acc[i][0][3]};
+            emit(x, (wm * FM + i) * 16 + lrow, wn * 16 + quarter * 4);
+        }
+    } else {
+        // Four blocks at a time, exchanged so that quarter q of the wavefront has 16 columns of block q's rows: blocks (i, j) to (i, j + 3),
+        // or, of two columns of blocks, (i, 0), (i, 1), (i + 1, 0), (i + 1, 1).
+        constexpr int GI = FN >= 4 ? 1 : 2, GJ = 4 / GI;
+        static_assert(FM % GI == 0 && FN % GJ == 0, "");
+#pragma unroll
+        for (int i = 0; i < FM; i += GI)
+#pragma unroll
+            for (int j = 0; j < FN; j += GJ) {
+                int x[16];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t d[4] = {(uint32_t)acc[i][j][r], (uint32_t)acc[i][j + 1][r], (uint32_t)acc[i + (GI - 1)][GJ == 4 ? j + 2 : j][r],
+                                           (uint32_t)acc[i + (GI - 1)][GJ == 4 ? j + 3 : j + 1][r]};
+                    const exchanged_t e = exchange_quarters(d);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) x[4 * q + r] = e[q];
+                }
+                emit(x, (wm * FM + i + quarter / GJ) * 16 + lrow, (wn * FN + j + quarter % GJ) * 16);
+            }
+    }
+}
+
+template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE>
+hipError_t launch_tiles(const I8Args &args, I8Form form, hipStream_t stream) {
+    typedef I8Core<WM, WN, FM, FN, STAGES> C;
+    static thread_local int attr_device = -1;                // the attribute is per device (set again per thread: harmless)
+    int dev = -1;
+    if (hipError_t e = hipGetDevice(&dev)) return e;
+    if (attr_device != dev) {
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_i8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, MODE>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS_BYTES)) return e;
+        attr_device = dev;
+    }
+    const int64_t tiles = i8_tiles(MODE, form, args);
+    const TileMap map = MODE == I8Mode::kRows ? TileMap{} : make_tile_map((args.m + C::BM - 1) / C::BM, (args.n + C::BN - 1) / C::BN, (int)tiles);
+    hipLaunchKernelGGL((k_i8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, MODE>), dim3((unsigned)tiles), dim3(C::THREADS), C::LDS_BYTES, stream, args, map);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_i8_product(I8Mode mode, const I8Args &args, I8Form form, hipStream_t stream) {
+    return mode == I8Mode::kDense ? launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kDense>(args, form, stream)
+         : mode == I8Mode::kRows  ? launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kRows>(args, form, stream)
+                                  : launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kSums>(args, form, stream);
+}
+
+}  // namespace oz2

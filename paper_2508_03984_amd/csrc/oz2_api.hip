@@ -1190,7 +1190,7 @@ oz2_status i8_convert(I8Quantize &p, const oz2_i8 *as_is, const oz2_i8 *transpos
 }
 
 oz2_status i8_launch(I8Mode mode, const I8Args &args, I8Form form, hipStream_t stream) {
-    if (i8_tiles(mode, form, args) * 256 >= kMaxThreads) return OZ2_UNSUPPORTED;
+    if (i8_tiles(mode, mode == I8Mode::kSums ? I8Form::kSmall : form, args) * 256 >= kMaxThreads) return OZ2_UNSUPPORTED;
     OZ2_TRY(launch_i8_product(mode, args, form, stream));
     return OZ2_OK;
 }
@@ -1269,7 +1269,7 @@ oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t group
     if (rows > kF8MaxRows || i8_too_many(groups, n) || k > kI8MaxK) return OZ2_UNSUPPORTED;
     args.m = (int)rows; args.n = (int)n; args.k = (int)k;
     args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
-    return i8_launch(I8Mode::kRows, args, I8Form::kSmall, stream);
+    return i8_launch(I8Mode::kRows, args, i8_grouped_form(I8Mode::kRows, args), stream);
 }
 
 oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
@@ -1287,7 +1287,7 @@ oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t group
     }
     args.m = (int)m; args.n = (int)n; args.k = (int)rows;
     args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
-    return i8_launch(I8Mode::kSums, args, I8Form::kSmall, stream);
+    return i8_launch(I8Mode::kSums, args, i8_grouped_form(I8Mode::kSums, args), stream);
 }
 
 size_t oz2_i8_workspace_bytes(int64_t m, int64_t n, int64_t k) {

@@ -36,6 +36,7 @@ struct I8Args {
     int m, n, k;                           // kRows: m = rows of A at most; kSums: k = the most that a group may have
     I8Groups groups;
     int ranges, kb_each;                   // kDense: K ranges and their length in blocks
+    int only_short;                        // kSums: groups that large tiles take have been served
     F8Out out;                             // (planes hold int32 sums)
 };
 
@@ -59,16 +60,34 @@ inline int64_t i8_grouped_cols(int64_t rows, int64_t groups) { return rows / kI8
 // Units of `each` rows that the rows of all groups have at most, each group's last one counted whole.
 inline int64_t i8_most_units(int64_t rows, int64_t groups, int64_t each) { return rows / each + std::min(groups, rows); }
 
-enum class I8Form { kSmall };
-inline int i8_tile_rows(I8Form) { return 64; }
-inline int i8_tile_cols(I8Form) { return 64; }
+// Tiles of C of 64 x 64 (oz2_i8_gemm.hip) or 256 x 256 (oz2_i8_wide.hip).
+enum class I8Form { kSmall, kLarge };
+inline int i8_tile_rows(I8Form form) { return form == I8Form::kLarge ? 256 : 64; }
+inline int i8_tile_cols(I8Form form) { return form == I8Form::kLarge ? 256 : 64; }
+constexpr int kI8WideBlocks = 3;           // what the kernel of large tiles needs of k, and one whole tile
+constexpr int kI8WideGroups = 1024;        // and the most groups that it keeps in LDS
+// kSums: groups that it takes; the other ones are left to small tiles.
+OZ2_HOST_DEVICE inline bool i8_by_large_tiles(int rows) { return rows > (kI8WideBlocks - 1) * kI8Block && rows <= kI8MaxK; }
+// Whether large tiles can serve a call at all.
+inline bool i8_large_possible(I8Mode mode, const I8Args &a) {
+    return a.m >= 256 && a.n >= 256 && (mode == I8Mode::kDense || a.groups.groups <= kI8WideGroups) && (mode == I8Mode::kSums || i8_blocks(a.k) >= kI8WideBlocks);
+}
 
 struct I8Plan {
     I8Form form;
     int ranges, kb_each;                   // K ranges, and blocks of each
     size_t plane_bytes;                    // workspace for the planes of the ranges (0: none needed)
 };
-inline I8Plan i8_plan(int64_t, int64_t, int64_t k) { return I8Plan{I8Form::kSmall, 1, (int)std::max<int64_t>(i8_blocks(k), 1), 0}; }
+inline I8Plan i8_plan(int64_t m, int64_t n, int64_t k) {
+    const bool large = m >= 256 && n >= 256 && i8_blocks(k) >= kI8WideBlocks && f8_ceil(m, 256) * f8_ceil(n, 256) >= 64;
+    return I8Plan{large ? I8Form::kLarge : I8Form::kSmall, 1, (int)std::max<int64_t>(i8_blocks(k), 1), 0};
+}
+// Products by group.
+inline I8Form i8_grouped_form(I8Mode mode, const I8Args &a) {
+    const int64_t tiles = mode == I8Mode::kRows ? i8_most_units(a.groups.rows, a.groups.groups, 256) : f8_ceil(a.m, 256) * a.groups.groups;
+    const int64_t mean = a.groups.rows / a.groups.groups;
+    return i8_large_possible(mode, a) && tiles * f8_ceil(a.n, 256) >= 64 && mean >= 256 ? I8Form::kLarge : I8Form::kSmall;
+}
 inline int64_t i8_plane_ld(int64_t n) { return f8_ceil(n, 16) * 16; }
 
 // Workgroups of a launch.
@@ -98,7 +117,8 @@ inline int64_t i8_quantize_threads(const I8Quantize &p) {
 }
 
 #if defined(__HIPCC__)
-hipError_t launch_i8_product(I8Mode mode, const I8Args &args, I8Form form, hipStream_t stream);
+hipError_t launch_i8_wide(I8Mode mode, const I8Args &args, hipStream_t stream);
+hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream);
 hipError_t launch_i8_quantize(const I8Quantize &args, int type, hipStream_t stream);
 #endif
 

@@ -96,6 +96,7 @@ __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, i
             t.c_row = row0;
         } else {
             const I8Span span = i8_span(p.groups, s);
+            if (p.only_short && i8_by_large_tiles(span.hi - span.lo)) return false;
             first = i8_first_col(span);
             scales_a = s * p.A.ld_scale;
             scales_b = s * p.B.ld_scale;
@@ -304,7 +305,13 @@ hipError_t launch_tiles(const I8Args &args, I8Form form, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_i8_product(I8Mode mode, const I8Args &args, I8Form form, hipStream_t stream) {
+hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream) {
+    if (form == I8Form::kLarge) {
+        if (hipError_t e = launch_i8_wide(mode, args, stream)) return e;
+        if (mode != I8Mode::kSums) return hipSuccess;
+        args.only_short = 1;
+        form = I8Form::kSmall;
+    }
     return mode == I8Mode::kDense ? launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kDense>(args, form, stream)
          : mode == I8Mode::kRows  ? launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kRows>(args, form, stream)
                                   : launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kSums>(args, form, stream);

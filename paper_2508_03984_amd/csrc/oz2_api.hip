@@ -1190,7 +1190,7 @@ oz2_status i8_convert(I8Quantize &p, const oz2_i8 *as_is, const oz2_i8 *transpos
 }
 
 oz2_status i8_launch(I8Mode mode, const I8Args &args, I8Form form, hipStream_t stream) {
-    if (i8_tiles(mode, mode == I8Mode::kSums ? I8Form::kSmall : form, args) * 256 >= kMaxThreads) return OZ2_UNSUPPORTED;
+    if (i8_tiles(mode, mode == I8Mode::kSums ? I8Form::kSmall : form, args) * (form == I8Form::kThin ? 512 : 256) >= kMaxThreads) return OZ2_UNSUPPORTED;
     OZ2_TRY(launch_i8_product(mode, args, form, stream));
     return OZ2_OK;
 }

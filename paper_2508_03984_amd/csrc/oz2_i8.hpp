@@ -60,10 +60,12 @@ inline int64_t i8_grouped_cols(int64_t rows, int64_t groups) { return rows / kI8
 // Units of `each` rows that the rows of all groups have at most, each group's last one counted whole.
 inline int64_t i8_most_units(int64_t rows, int64_t groups, int64_t each) { return rows / each + std::min(groups, rows); }
 
-// Tiles of C of 64 x 64 (oz2_i8_gemm.hip) or 256 x 256 (oz2_i8_wide.hip).
-enum class I8Form { kSmall, kLarge };
-inline int i8_tile_rows(I8Form form) { return form == I8Form::kLarge ? 256 : 64; }
-inline int i8_tile_cols(I8Form form) { return form == I8Form::kLarge ? 256 : 64; }
+// kThin: few rows (of a group), B read once into registers, 16 columns of C (of a group) to a workgroup (oz2_i8_thin.hip).  The others tiles of C
+// of 64 x 64 (oz2_i8_gemm.hip) or 256 x 256 (oz2_i8_wide.hip).
+enum class I8Form { kThin, kSmall, kLarge };
+inline int i8_tile_rows(I8Form form) { return form == I8Form::kThin ? 1 << 30 : form == I8Form::kLarge ? 256 : 64; }
+inline int i8_tile_cols(I8Form form) { return form == I8Form::kThin ? 16 : form == I8Form::kLarge ? 256 : 64; }
+constexpr int kI8ThinRows = 64;
 constexpr int kI8WideBlocks = 3;           // what the kernel of large tiles needs of k, and one whole tile
 constexpr int kI8WideGroups = 1024;        // and the most groups that it keeps in LDS
 // kSums: groups that it takes; the other ones are left to small tiles.
@@ -80,12 +82,13 @@ struct I8Plan {
 };
 inline I8Plan i8_plan(int64_t m, int64_t n, int64_t k) {
     const bool large = m >= 256 && n >= 256 && i8_blocks(k) >= kI8WideBlocks && f8_ceil(m, 256) * f8_ceil(n, 256) >= 64;
-    return I8Plan{large ? I8Form::kLarge : I8Form::kSmall, 1, (int)std::max<int64_t>(i8_blocks(k), 1), 0};
+    return I8Plan{m <= kI8ThinRows && k > 0 ? I8Form::kThin : large ? I8Form::kLarge : I8Form::kSmall, 1, (int)std::max<int64_t>(i8_blocks(k), 1), 0};
 }
 // Products by group.
 inline I8Form i8_grouped_form(I8Mode mode, const I8Args &a) {
     const int64_t tiles = mode == I8Mode::kRows ? i8_most_units(a.groups.rows, a.groups.groups, 256) : f8_ceil(a.m, 256) * a.groups.groups;
     const int64_t mean = a.groups.rows / a.groups.groups;
+    if (mode == I8Mode::kRows && a.k > 0 && mean <= 32) return I8Form::kThin;
     return i8_large_possible(mode, a) && tiles * f8_ceil(a.n, 256) >= 64 && mean >= 256 ? I8Form::kLarge : I8Form::kSmall;
 }
 inline int64_t i8_plane_ld(int64_t n) { return f8_ceil(n, 16) * 16; }
@@ -117,6 +120,7 @@ inline int64_t i8_quantize_threads(const I8Quantize &p) {
 }
 
 #if defined(__HIPCC__)
+hipError_t launch_i8_thin(I8Mode mode, const I8Args &args, hipStream_t stream);
 hipError_t launch_i8_wide(I8Mode mode, const I8Args &args, hipStream_t stream);
 hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream);
 hipError_t launch_i8_quantize(const I8Quantize &args, int type, hipStream_t stream);

@@ -80,4 +80,18 @@ __device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t pe
 // First column of a group whose rows lie side by side with the others'.
 __device__ __forceinline__ int64_t i8_first_col(const I8Span &s) { return (int64_t)(s.lo / kI8Block + s.group) * kI8Block; }
 
+// Entries of C from sums: N of a row, of which `valid` exist, with the scale of the row and those of the columns.
+template <int N>
+__device__ __forceinline__ void i8_finish_row(const F8Out &o, int64_t at, const int (&sum)[N], float a, const float *b, int valid) {
+    float x[N], scale[N];
+    if (valid >= N) __builtin_memcpy(scale, b, sizeof scale);
+    else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) scale[i] = b[min(i, valid - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (float)sum[i] * a * scale[i];
+    f8_update_row<N>(o, at, x, valid);
+}
+
 }  // namespace oz2

@@ -114,28 +114,6 @@ __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, i
     return true;
 }
 
-// The entries of C from sums: N of a row, of which `valid` exist, with the scale of the row and those of the columns.
-template <int N>
-__device__ __forceinline__ void finish_row(const F8Out &o, int64_t at, const int (&sum)[N], float a, const float *b, int valid, bool lost, bool none) {
-    float x[N], scale[N];
-    if (none) {                                                            // (no scales either)
-        F8Out nothing = o;
-        nothing.alpha = 0.0f;                                              // no infinity or NaN from it
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = lost ? __builtin_nanf("") : 0.0f;
-        f8_update_row<N>(nothing, at, x, valid);
-        return;
-    }
-    if (valid >= N) __builtin_memcpy(scale, b, sizeof scale);
-    else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) scale[i] = b[min(i, valid - 1)];
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (float)sum[i] * a * scale[i];
-    f8_update_row<N>(o, at, x, valid);
-}
-
 template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE>
 __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, TileMap map) {
     typedef I8Core<WM, WN, FM, FN, STAGES> C;
@@ -255,7 +233,14 @@ __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, Ti
                 const f8_v4i w{x[i], x[i + 1], x[i + 2], x[i + 3]};
                 *reinterpret_cast<f8_v4i *>(to + i) = w;
             }
-        } else finish_row<N>(o, (t.c_row + row) * o.ldc + t.c_col + col, x, none ? 0.0f : t.scale_a[row], t.scale_b + col, valid, t.lost, none);
+        } else if (none) {                                                 // no scales either, and no infinity or NaN from alpha
+            float y[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i] = t.lost ? __builtin_nanf("") : 0.0f;
+            F8Out nothing = o;
+            nothing.alpha = 0.0f;
+            f8_update_row<N>(nothing, (t.c_row + row) * o.ldc + t.c_col + col, y, valid);
+        } else i8_finish_row<N>(o, (t.c_row + row) * o.ldc + t.c_col + col, x, t.scale_a[row], t.scale_b + col, valid);
     };
     if constexpr (FN == 1) {                                               // 4 numbers of a row per lane, as they are
 #pragma unroll
@@ -306,6 +291,7 @@ hipError_t launch_tiles(const I8Args &args, I8Form form, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream) {
+    if (form == I8Form::kThin) return launch_i8_thin(mode, args, stream);
     if (form == I8Form::kLarge) {
         if (hipError_t e = launch_i8_wide(mode, args, stream)) return e;
         if (mode != I8Mode::kSums) return hipSuccess;

@@ -311,3 +311,22 @@ def test_grouped_grad(offsets, m, n, dtype):
             want = alpha32 * summed + beta * old[i * m:(i + 1) * m]
             R.check(c[i * m:(i + 1) * m], want, R.bound(summed, want, dtype, alpha, beta))
         outside_kept(c, buf, before)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offsets", [list(range(40)) + [500], [0, 700] + list(range(701, 760)), [0] * 100 + [1] * 20 + [9], [4, 4, 4, 90, 90]], ids=["end", "start", "few", "one"])
+@pytest.mark.parametrize("n,k", [(16, 2048), (130, 515), (1000, 4100), (5, 70000)])
+def test_grouped_with_most_rows_in_one_group(offsets, n, k, dtype):
+    rows, groups, g = offsets[-1] + 3, len(offsets) - 1, gen(n + k)
+    a, b = operand(g, rows, k), operand(g, groups * n, k)
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    c, buf, before = output(g, rows, n, dtype)
+    old, alpha = c.double(), 2.0 ** -20
+    oz.oz2_i8_grouped_gemm(rows, n, k, groups, off, alpha, a, b, 0.0, c, c.stride(0))
+    for i in range(groups):
+        lo, hi = offsets[i], offsets[i + 1]
+        if lo < hi:
+            summed = R.product((a.q[lo:hi], a.scale[lo:hi]), (b.q[i * n:(i + 1) * n], b.scale[i * n:(i + 1) * n]))
+            R.check(c[lo:hi], alpha * summed, R.bound(summed, alpha * summed, dtype, alpha))
+    assert torch.equal(c[:offsets[0]].double(), old[:offsets[0]]) and torch.equal(c[offsets[-1]:].double(), old[offsets[-1]:])
+    outside_kept(c, buf, before)

@@ -1244,7 +1244,16 @@ oz2_status oz2_ctx_i8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, fl
     args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
     Ctx &g = resolve(ctx);
     std::lock_guard<std::mutex> lock(g.mu);
-    const I8Plan plan = i8_plan(m, n, k);
+    I8Plan plan = i8_plan(m, n, k);
+    args.ranges = plan.ranges;
+    if (i8_tiles(I8Mode::kDense, plan.form, args) * 512 >= kMaxThreads) return OZ2_UNSUPPORTED;
+    if (plan.ranges > 1) {
+        if (oz2_status st = f8_planes(g, plan.plane_bytes, &args.out.planes)) return st;
+        if (args.out.planes) {
+            args.out.ldp = i8_plane_ld(n);
+            args.out.plane = m * args.out.ldp;
+        } else plan = i8_plan_one_range(m, n, k);
+    }
     args.ranges = plan.ranges;
     args.kb_each = plan.kb_each;
     return i8_launch(I8Mode::kDense, args, plan.form, stream);

@@ -61,10 +61,10 @@ inline int64_t i8_grouped_cols(int64_t rows, int64_t groups) { return rows / kI8
 inline int64_t i8_most_units(int64_t rows, int64_t groups, int64_t each) { return rows / each + std::min(groups, rows); }
 
 // kThin: few rows (of a group), B read once into registers, 16 columns of C (of a group) to a workgroup (oz2_i8_thin.hip).  The others tiles of C
-// of 64 x 64 (oz2_i8_gemm.hip) or 256 x 256 (oz2_i8_wide.hip).
-enum class I8Form { kThin, kSmall, kLarge };
+// of 64 x 64, 64 x 128 (oz2_i8_gemm.hip) or 256 x 256 (oz2_i8_wide.hip); kDense may cut k into ranges whose sums are added by a second kernel.
+enum class I8Form { kThin, kSmall, kMiddle, kLarge };
 inline int i8_tile_rows(I8Form form) { return form == I8Form::kThin ? 1 << 30 : form == I8Form::kLarge ? 256 : 64; }
-inline int i8_tile_cols(I8Form form) { return form == I8Form::kThin ? 16 : form == I8Form::kLarge ? 256 : 64; }
+inline int i8_tile_cols(I8Form form) { return form == I8Form::kThin ? 16 : form == I8Form::kLarge ? 256 : form == I8Form::kMiddle ? 128 : 64; }
 constexpr int kI8ThinRows = 64;
 constexpr int kI8WideBlocks = 3;           // what the kernel of large tiles needs of k, and one whole tile
 constexpr int kI8WideGroups = 1024;        // and the most groups that it keeps in LDS
@@ -79,10 +79,58 @@ struct I8Plan {
     I8Form form;
     int ranges, kb_each;                   // K ranges, and blocks of each
     size_t plane_bytes;                    // workspace for the planes of the ranges (0: none needed)
+    double us;                             // what it is expected to take
 };
+inline int64_t i8_plane_ld(int64_t n) { return f8_ceil(n, 16) * 16; }
+
+struct I8Cost {
+    I8Form form;
+    int share;
+    double once, per_tile, first_block, further_block;         // per block: the first tile of a unit, each further one
+};
+constexpr I8Cost kI8Costs[3] = {{I8Form::kSmall, 4, 3.5, 2.2, 0.285, 0.125}, {I8Form::kMiddle, 2, 3.2, 2.8, 0.42, 0.18}, {I8Form::kLarge, 1, 9.0, 3.0, 1.45, 0.0}};
+constexpr double kI8RangesOnce = 3.0, kI8PlaneBytesPerUs = 4.0e6;   // the second kernel; planes are written and read
+constexpr double kI8BytesPerUs = 5.2e6;                        // from HBM
+constexpr int kI8MaxRanges = 16;
+
+inline double i8_thin_us(int64_t m, int64_t n, int64_t k) {
+    const int64_t rounds = f8_ceil(f8_ceil(n, 16), 256), computed = m <= 16 ? 16 : m <= 32 ? 32 : 64;
+    return std::max(3.0 + rounds * k * ((m + computed) / 2.0 + 8) / 2.8e4, 1.0 + (double)n * k / kI8BytesPerUs);
+}
+
 inline I8Plan i8_plan(int64_t m, int64_t n, int64_t k) {
-    const bool large = m >= 256 && n >= 256 && i8_blocks(k) >= kI8WideBlocks && f8_ceil(m, 256) * f8_ceil(n, 256) >= 64;
-    return I8Plan{m <= kI8ThinRows && k > 0 ? I8Form::kThin : large ? I8Form::kLarge : I8Form::kSmall, 1, (int)std::max<int64_t>(i8_blocks(k), 1), 0};
+    const int64_t blocks = i8_blocks(k);
+    I8Plan best{I8Form::kSmall, 1, (int)std::max<int64_t>(blocks, 1), 0, 1e30};
+    if (m <= kI8ThinRows && k > 0) {
+        best.form = I8Form::kThin;
+        best.us = i8_thin_us(m, n, k);
+    }
+    for (const I8Cost &c : kI8Costs) {
+        if (c.form == I8Form::kLarge && (m < 256 || n < 256)) continue;
+        const int64_t tiles = f8_ceil(m, i8_tile_rows(c.form)) * f8_ceil(n, i8_tile_cols(c.form)), round = 256 * c.share;
+        int64_t last = 0;
+        for (int64_t asked = 1; asked <= std::min<int64_t>(std::max<int64_t>(blocks, 1), kI8MaxRanges); ++asked) {
+            const int64_t each = std::max<int64_t>(f8_ceil(blocks, asked), 1), ranges = std::max<int64_t>(f8_ceil(blocks, each), 1);
+            if (ranges == last) continue;
+            last = ranges;
+            if (c.form == I8Form::kLarge && blocks - (ranges - 1) * each < kI8WideBlocks) continue;
+            const int64_t items = tiles * ranges, rounds = items / round, rest = f8_ceil(items - rounds * round, 256);
+            const size_t planes = ranges == 1 ? 0 : (size_t)ranges * (size_t)m * (size_t)i8_plane_ld(n) * 4;
+            double us = c.once + rounds * (c.per_tile + each * (c.first_block + (c.share - 1) * c.further_block));
+            if (rest) us += c.per_tile + each * (c.first_block + (rest - 1) * c.further_block);
+            us = std::max(us, 3.0 + (double)(m + n) * k / kI8BytesPerUs) + (planes ? kI8RangesOnce + planes / kI8PlaneBytesPerUs : 0.0);
+            if (us < best.us) best = I8Plan{c.form, (int)ranges, (int)each, planes, us};
+        }
+    }
+    return best;
+}
+// The same without planes.
+inline I8Plan i8_plan_one_range(int64_t m, int64_t n, int64_t k) {
+    I8Plan p = i8_plan(m, n, k);
+    p.ranges = 1;
+    p.kb_each = (int)std::max<int64_t>(i8_blocks(k), 1);
+    p.plane_bytes = 0;
+    return p;
 }
 // Products by group.
 inline I8Form i8_grouped_form(I8Mode mode, const I8Args &a) {
@@ -91,7 +139,6 @@ inline I8Form i8_grouped_form(I8Mode mode, const I8Args &a) {
     if (mode == I8Mode::kRows && a.k > 0 && mean <= 32) return I8Form::kThin;
     return i8_large_possible(mode, a) && tiles * f8_ceil(a.n, 256) >= 64 && mean >= 256 ? I8Form::kLarge : I8Form::kSmall;
 }
-inline int64_t i8_plane_ld(int64_t n) { return f8_ceil(n, 16) * 16; }
 
 // Workgroups of a launch.
 inline int64_t i8_tiles(I8Mode mode, I8Form form, const I8Args &a) {
@@ -102,19 +149,49 @@ inline int64_t i8_tiles(I8Mode mode, I8Form form, const I8Args &a) {
 
 // Conversions: numbers of a row that 256 threads hold, 8 each and 1, 2, 4 or 8 times.
 constexpr int kI8RowThreads = 256, kI8MostHeld = 8 * 8 * kI8RowThreads;
-constexpr int kI8ColumnRows = 128, kI8ColumnCols = 512;         // of a workgroup that takes maxima of columns
+constexpr int kI8ColumnThreads = 512;                           // of a workgroup that takes maxima of columns
 constexpr int kI8TileThreads = 512;                             // of a tile of 128 x 128 that is turned
+// Workgroups for the rows of all groups in units of `each`, `parts` to a unit.
+inline int64_t i8_quantize_pieces(const I8Groups &g, int64_t each, int64_t parts) {
+    return f8_ceil((g.offsets ? i8_most_units(g.rows, g.groups, each) : g.groups * f8_ceil(g.each, each)) * parts, 8) * 8;
+}
 
-// Threads of the largest launch of a conversion.
-inline int64_t i8_quantize_units(const I8Groups &g, int64_t each) { return g.offsets ? i8_most_units(g.rows, g.groups, each) : g.groups * f8_ceil(g.each, each); }
+// lanes: threads to a row that is held (0: it is read twice); rows_each: rows of a workgroup that converts them and takes the maxima of columns with them, 0: it
+// takes none; columns_each: rows of one that takes maxima of columns only, 0: there is none.
+struct I8ConvertPlan {
+    int lanes, rows_each, columns_each;
+};
+inline I8ConvertPlan i8_convert_plan(const I8Quantize &p) {
+    const int64_t rows = p.groups.rows, groups = p.groups.groups;
+    I8ConvertPlan plan{p.cols <= 32 ? 4 : p.cols <= 128 ? 16 : p.cols <= 512 ? 64 : p.cols <= kI8MostHeld ? 256 : 0, 0, 0};
+    if (p.cols > 2048 && plan.lanes && rows <= 512) plan.lanes = 1024;
+    if (!p.qt) return plan;
+    // Atomic maxima of one scale take about 20 ns each, one after the other, so at most 128 workgroups raise the same ones (1024 did: 16384 x 512 bf16 22 us, now 7).
+    // With the rows (one read less) where that leaves workgroups enough for the device, or little work in all.  Together | apart, us: 8 of 4096 x 2048 f32 126 | 152,
+    // 200 x 400 f32 10.1 | 14.0; 4096 x 4096 bf16 50 | 35, 16384 x 4096 150 | 96.
+    const int64_t subs = plan.lanes ? kI8RowThreads / std::min(plan.lanes, kI8RowThreads) : 1;
+    const bool fused = p.q && plan.lanes && plan.lanes <= kI8RowThreads && (groups >= 6 || rows <= 512);
+    const auto whole = [](int64_t each, int64_t of) { return (int)(f8_ceil(std::max<int64_t>(each, 1), of) * of); };
+    if (fused) plan.rows_each = whole(std::max(f8_ceil(rows, 128 * groups), f8_ceil(rows, 1024)), subs);
+    else {
+        const int64_t lanes = p.cols <= 32 ? 4 : p.cols <= 128 ? 16 : 64, parts = f8_ceil(p.cols, lanes * 8);
+        plan.columns_each = whole(std::max(f8_ceil(rows, 128 * groups), f8_ceil(rows * parts, 1024)), 4 * kI8ColumnThreads / lanes);
+    }
+    return plan;
+}
+// Threads of the largest launch.
 inline int64_t i8_quantize_threads(const I8Quantize &p) {
+    const I8ConvertPlan plan = i8_convert_plan(p);
     const int64_t rows = p.groups.rows;
     int64_t most = 0;
-    if (p.q) most = p.cols <= 512 ? f8_ceil(rows, 4) * kI8RowThreads : rows * (p.cols <= kI8MostHeld ? kI8RowThreads : 1024);
+    if (p.q)
+        most = plan.rows_each ? i8_quantize_pieces(p.groups, plan.rows_each, 1) * kI8RowThreads
+               : plan.lanes   ? f8_ceil(rows * plan.lanes, kI8RowThreads) * kI8RowThreads
+                              : rows * 1024;
     if (p.qt) {
         most = std::max(most, f8_ceil(p.side_by_side ? p.cols : p.cols * p.groups.groups, 256) * 256 * (p.side_by_side ? p.groups.groups : 1));
-        most = std::max(most, f8_ceil(i8_quantize_units(p.groups, kI8ColumnRows) * f8_ceil(p.cols, kI8ColumnCols), 8) * 8 * 256);
-        most = std::max(most, f8_ceil(i8_quantize_units(p.groups, 128) * f8_ceil(p.cols, 128), 8) * 8 * kI8TileThreads);
+        if (plan.columns_each) most = std::max(most, i8_quantize_pieces(p.groups, plan.columns_each, f8_ceil(p.cols, p.cols <= 32 ? 32 : p.cols <= 128 ? 128 : 512)) * kI8ColumnThreads);
+        most = std::max(most, i8_quantize_pieces(p.groups, 128, f8_ceil(p.cols, 128)) * kI8TileThreads);
     }
     return most;
 }

@@ -15,14 +15,18 @@ __device__ __forceinline__ I8Span i8_span(const I8Groups &s, int g) {
     return I8Span{g, lo, min(max(s.offsets[g + 1], lo), s.rows)};
 }
 
-__device__ __forceinline__ uint32_t i8_running_sum(uint32_t x, int lane) {
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) {
-        const uint32_t below = __shfl_up(x, by);
-        x += lane >= by ? below : 0;
-    }
-    return x;
+// The sums over lanes 0 to l, by moves within rows of 16 lanes, then of the rows' last lanes.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ uint32_t i8_plus_moved(uint32_t x) { return x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CONTROL, ROWS, 0xf, false); }
+__device__ __forceinline__ uint32_t i8_running_sum(uint32_t x) {
+    x = i8_plus_moved<0x111, 0xf>(x);                          // from the lane before, 2, 4, 8 before
+    x = i8_plus_moved<0x112, 0xf>(x);
+    x = i8_plus_moved<0x114, 0xf>(x);
+    x = i8_plus_moved<0x118, 0xf>(x);
+    x = i8_plus_moved<0x142, 0xa>(x);                          // lane 15 to lanes 16 .. 31, lane 47 to 48 .. 63
+    return i8_plus_moved<0x143, 0xc>(x);                       // lane 31 to the upper half
 }
+__device__ __forceinline__ uint32_t i8_last(uint32_t running) { return (uint32_t)__builtin_amdgcn_readlane((int)running, 63); }
 
 // The groups cut into units of `each` rows, `per` pieces of work to a unit.  A workgroup's place among them, from its id: each of the 8 XCDs, to which ids go in
 // turns, has neighbouring pieces of one group, which share their operands in its L2.  False if there is none for the id.  A wavefront does this together, 64 groups
@@ -47,9 +51,9 @@ __device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t pe
         const I8Span span = i8_span(s, g);
         return (uint32_t)(span.hi - span.lo + each - 1) / (uint32_t)each;
     };
-    uint32_t total = 0, first = count(lane), running = i8_running_sum(first, lane);
-    total = (uint32_t)__shfl((int)running, 63);
-    for (int g0 = 64; g0 < s.groups; g0 += 64) total += (uint32_t)__shfl((int)i8_running_sum(count(g0 + lane), lane), 63);
+    uint32_t total = 0, first = count(lane), running = i8_running_sum(first);
+    total = i8_last(running);
+    for (int g0 = 64; g0 < s.groups; g0 += 64) total += i8_last(i8_running_sum(count(g0 + lane)));
     total *= per;
     const uint32_t share = (total + 7) / 8, place = (id & 7) * share + (id >> 3);
     if ((id >> 3) >= share || place >= total) return false;    // uniform
@@ -58,7 +62,7 @@ __device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t pe
     for (int g0 = 0; g0 < s.groups; g0 += 64) {
         if (g0) {
             first = count(g0 + lane);
-            running = i8_running_sum(first, lane);
+            running = i8_running_sum(first);
         }
         const uint64_t beyond = __ballot(before + running > unit);
         if (beyond) {
@@ -72,7 +76,7 @@ __device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t pe
             out.piece = (uint32_t)__builtin_amdgcn_readfirstlane((int)out.piece);
             return out.piece < out.units * per;
         }
-        before += (uint32_t)__shfl((int)running, 63);
+        before += i8_last(running);
     }
     return false;
 }

@@ -24,8 +24,8 @@ struct I8Core {
     static constexpr int BM = WM * FM * 16, BN = WN * FN * 16;
     static constexpr int ROWS = BM + BN, STAGE_BYTES = ROWS * 128;
     static constexpr int LOADS = ROWS / 8 / WAVES, A_LOADS = BM / 8 / WAVES;
-    static constexpr size_t LDS_BYTES = STAGES * STAGE_BYTES;
-    static_assert(BM <= THREADS && WAVES % 2 == 0 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && LOADS * (STAGES - 2) < 64, "");
+    static constexpr size_t LDS_BYTES = STAGES * STAGE_BYTES + ROWS * 4;  // the scales of the rows behind the stages
+    static_assert(ROWS <= THREADS && WAVES % 2 == 0 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0 && LOADS * (STAGES - 2) < 64, "");
 };
 
 // At most N loads of this wavefront outstanding, for one of several N; own LDS reads done; then all wavefronts meet.
@@ -123,6 +123,11 @@ __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, Ti
     if (!find_tile<MODE, C::BM, C::BN>(p, map, (int)blockIdx.x, t)) return;
     const int KB = (t.k + kI8Block - 1) / kI8Block, kb0 = t.kb0, kb1 = t.kb1;
 
+    const bool none = kb0 >= kb1;
+    float scale = 0.0f;                                                    // of a row of A or B for each thread, which all need after the sums
+    if (!none && (int)threadIdx.x < C::ROWS)
+        scale = (int)threadIdx.x < C::BM ? t.scale_a[min((int)threadIdx.x, t.rows - 1)] : t.scale_b[min((int)threadIdx.x - C::BM, t.cols - 1)];
+
     // Load H of this wavefront takes the 8 rows from 8 (H WAVES + wave) on; a lane 16 bytes of one.
     const int chunk = (lane & 7) ^ ((wave & 1) * 4 + quarter);
     uint32_t offset[C::LOADS];
@@ -219,28 +224,34 @@ __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, Ti
         }
     }
 
-    const F8Out &o = p.out;
-    const bool none = kb0 >= kb1;
+    float *const scales = reinterpret_cast<float *>(i8_lds) + STAGES * C::STAGE_BYTES / 4;
+    if ((int)threadIdx.x < C::ROWS) scales[threadIdx.x] = scale;
+    __syncthreads();
+    F8Out o = p.out;
+    if (none) o.alpha = 0.0f;                                              // no infinity or NaN from it
     // N numbers of a row, at a column that is a multiple of N.
-    const auto emit = [&](const auto &x, int row, int col) {
-        constexpr int N = sizeof(x) / sizeof(x[0]);
+    const auto emit = [&](const auto &sum, int row, int col) {
+        constexpr int N = sizeof(sum) / sizeof(sum[0]);
         const int valid = row < t.rows ? t.cols - col : 0;
         if (valid <= 0) return;
         if (MODE == I8Mode::kDense && o.planes) {                          // (a plane's rows are stored to a multiple of 16)
             int32_t *const to = reinterpret_cast<int32_t *>(o.planes) + t.range * o.plane + (t.c_row + row) * o.ldp + t.c_col + col;
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
-                const f8_v4i w{x[i], x[i + 1], x[i + 2], x[i + 3]};
+                const f8_v4i w{sum[i], sum[i + 1], sum[i + 2], sum[i + 3]};
                 *reinterpret_cast<f8_v4i *>(to + i) = w;
             }
-        } else if (none) {                                                 // no scales either, and no infinity or NaN from alpha
-            float y[N];
+            return;
+        }
+        float x[N];
+        const float a = t.lost ? __builtin_nanf("") : scales[row];
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = t.lost ? __builtin_nanf("") : 0.0f;
-            F8Out nothing = o;
-            nothing.alpha = 0.0f;
-            f8_update_row<N>(nothing, (t.c_row + row) * o.ldc + t.c_col + col, y, valid);
-        } else i8_finish_row<N>(o, (t.c_row + row) * o.ldc + t.c_col + col, x, t.scale_a[row], t.scale_b + col, valid);
+        for (int i = 0; i < N; i += 4) {
+            const f8_v4f b = *reinterpret_cast<const f8_v4f *>(scales + C::BM + col + i);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[i + u] = (float)sum[i + u] * a * b[u];
+        }
+        f8_update_row<N>(o, (t.c_row + row) * o.ldc + t.c_col + col, x, valid);
     };
     if constexpr (FN == 1) {                                               // 4 numbers of a row per lane, as they are
 #pragma unroll
@@ -288,19 +299,53 @@ hipError_t launch_tiles(const I8Args &args, I8Form form, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// The sums of the K ranges, and what the tiles do with a sum.  A thread has 4 columns of a row.
+__global__ __launch_bounds__(256) void k_i8_ranges(I8Args p) {
+    const int per_row = (p.n + 3) / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / per_row;
+    if (row >= p.m) return;
+    const int col = (int)(id - row * per_row) * 4, valid = p.n - col;
+    const int32_t *const from = reinterpret_cast<const int32_t *>(p.out.planes) + row * p.out.ldp + col;
+    f8_v4i s{0, 0, 0, 0};
+    for (int r0 = 0; r0 < p.ranges; r0 += 4) {                 // four loads at a time: one after the other costs a way to memory each
+        f8_v4i x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = *reinterpret_cast<const f8_v4i *>(from + (int64_t)min(r0 + r, p.ranges - 1) * p.out.plane);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r0 + r < p.ranges) s += x[r];
+    }
+    const int sum[4] = {s[0], s[1], s[2], s[3]};
+    i8_finish_row<4>(p.out, row * p.out.ldc + col, sum, p.A.scale[row], p.B.scale + col, valid);
+}
+
+// Tiles of 64 x 64 by four wavefronts of 32 x 32, with as many stages as leave all tiles of a call on the device at once, two at least; of 64 x 128 with three.
+template <I8Mode MODE>
+hipError_t launch_form(const I8Args &args, I8Form form, hipStream_t stream) {
+    const int64_t tiles = i8_tiles(MODE, form, args);
+    if (hipError_t e = form == I8Form::kLarge    ? launch_i8_wide(MODE, args, stream)
+                       : form == I8Form::kMiddle ? launch_tiles<2, 2, 2, 4, 3, 2, MODE>(args, form, stream)
+                       : tiles <= 512            ? launch_tiles<2, 2, 2, 2, 4, 2, MODE>(args, form, stream)
+                       : tiles <= 768            ? launch_tiles<2, 2, 2, 2, 3, 3, MODE>(args, form, stream)
+                                                 : launch_tiles<2, 2, 2, 2, 2, 4, MODE>(args, form, stream)) return e;
+    if (MODE != I8Mode::kDense || args.ranges <= 1) return hipSuccess;
+    const int64_t threads = (int64_t)args.m * ((args.n + 3) / 4);
+    hipLaunchKernelGGL(k_i8_ranges, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, args);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream) {
     if (form == I8Form::kThin) return launch_i8_thin(mode, args, stream);
-    if (form == I8Form::kLarge) {
+    if (form == I8Form::kLarge && mode == I8Mode::kSums) {
         if (hipError_t e = launch_i8_wide(mode, args, stream)) return e;
-        if (mode != I8Mode::kSums) return hipSuccess;
         args.only_short = 1;
         form = I8Form::kSmall;
     }
-    return mode == I8Mode::kDense ? launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kDense>(args, form, stream)
-         : mode == I8Mode::kRows  ? launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kRows>(args, form, stream)
-                                  : launch_tiles<2, 2, 2, 2, 2, 4, I8Mode::kSums>(args, form, stream);
+    return mode == I8Mode::kDense ? launch_form<I8Mode::kDense>(args, form, stream)
+         : mode == I8Mode::kRows  ? launch_form<I8Mode::kRows>(args, form, stream)
+                                  : launch_form<I8Mode::kSums>(args, form, stream);
 }
 
 }  // namespace oz2

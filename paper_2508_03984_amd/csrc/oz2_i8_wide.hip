@@ -152,13 +152,13 @@ struct Wide {
                 const int g = g0 + lane;
                 I8Span span{0, 0, 0};
                 if (g < s.groups) span = i8_span(s, g);
-                const uint32_t running = before + i8_running_sum((uint32_t)(span.hi - span.lo + 255) / 256, lane);
+                const uint32_t running = before + i8_running_sum((uint32_t)(span.hi - span.lo + 255) / 256);
                 if (g < s.groups) {
                     group_rows()[g] = span.lo;
                     group_units()[g] = running;
                     if (g == s.groups - 1) group_rows()[g + 1] = span.hi;
                 }
-                before = (uint32_t)__shfl((int)running, 63);
+                before = i8_last(running);
             }
         }
         __syncthreads();

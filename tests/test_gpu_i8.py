@@ -330,3 +330,28 @@ def test_grouped_with_most_rows_in_one_group(offsets, n, k, dtype):
             R.check(c[lo:hi], alpha * summed, R.bound(summed, alpha * summed, dtype, alpha))
     assert torch.equal(c[:offsets[0]].double(), old[:offsets[0]]) and torch.equal(c[offsets[-1]:].double(), old[offsets[-1]:])
     outside_kept(c, buf, before)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(100, 100, 20000), (54, 205, 13245), (3, 16, 40000), (512, 500, 4100), (1300, 1000, 30001), (200, 1, 131071)])
+def test_product_in_ranges_of_k(m, n, k, dtype):
+    g = gen(k)
+    a, b = operand(g, m, k), operand(g, n, k)
+    summed = R.product((a.q, a.scale), (b.q, b.scale))
+    need = oz.oz2_i8_workspace_bytes(m, n, k)
+    assert need > 0
+    own, small = oz.Context(), oz.Context()
+    room = torch.empty(1 << 12, dtype=torch.uint8, device="cuda")
+    oz.oz2_ctx_set_workspace(small, room)       # no room for planes: one range
+    for alpha, beta in ((2.0 ** -20, 0.0), (-2.0 ** -19, 0.75)):
+        results = []
+        for ctx in (None, own, small):
+            gen_c = gen(7)
+            c, buf, before = output(gen_c, m, n, dtype)
+            old = c.double()
+            oz.oz2_ctx_i8_gemm(ctx, m, n, k, alpha, a, b, beta, c, c.stride(0))
+            want = alpha * summed + beta * old
+            R.check(c, want, R.bound(summed, want, dtype, alpha, beta))
+            results.append(c.clone())
+            outside_kept(c, buf, before)
+        assert torch.equal(results[0], results[1]) and torch.equal(results[0], results[2])  # (integer sums are exact in any order)

@@ -132,14 +132,31 @@ inline I8Plan i8_plan_one_range(int64_t m, int64_t n, int64_t k) {
     p.plane_bytes = 0;
     return p;
 }
-// Products by group.
+// Products by group, from the mean of their rows, by the costs of single ones (us; small | middle | large): kRows, 64 groups, 2048 x 2048, mean 24 51 | 44 | 67, 64 68 | 56 | 69, 256 160 | 132 | 102;
+// 8 groups, 2048 x 1024, mean 100 6.8 | 7.2 | 17, 800 30 | 30 | 23; 8 groups, 8192 x 4096, mean 256 147 | 122 | 100.  kSums, 8 groups, 4096 x 2048, mean 400 74 | 72 | 82, 800
+// 112 | 102 | 95, 2000 214 | 190 | 142; 16 groups, 256 x 512, mean 800 9.2 | 11.3 | 32.
 inline I8Form i8_grouped_form(I8Mode mode, const I8Args &a) {
-    const int64_t tiles = mode == I8Mode::kRows ? i8_most_units(a.groups.rows, a.groups.groups, 256) : f8_ceil(a.m, 256) * a.groups.groups;
-    const int64_t mean = a.groups.rows / a.groups.groups;
-    if (mode == I8Mode::kRows && a.k > 0 && mean <= 32) return I8Form::kThin;
-    return i8_large_possible(mode, a) && tiles * f8_ceil(a.n, 256) >= 64 && mean >= 256 ? I8Form::kLarge : I8Form::kSmall;
+    const int64_t rows = a.groups.rows, groups = a.groups.groups, mean = rows / groups, sought = std::min(groups, rows);
+    // Thin | small: 64 groups, 4096 x 2048, 1 row 3.9 | 7.0, 32 rows 29 | 29, 256 rows 102 | 88; 4 groups, 512 x 512, 32 rows 3.1 | 4.1; 8 groups, 8192 x 4096, 8 rows 33 | 25.
+    if (mode == I8Mode::kRows && a.k > 0 && (mean < 2 || (mean <= 8 && groups * a.n * (int64_t)a.k <= 1 << 21))) return I8Form::kThin;
+    const int64_t blocks = mode == I8Mode::kRows ? i8_blocks(a.k) : i8_blocks(mean);
+    I8Form best = I8Form::kSmall;
+    double least = 1e30;
+    for (const I8Cost &c : kI8Costs) {
+        if (c.form == I8Form::kLarge && (!i8_large_possible(mode, a) || mean < (mode == I8Mode::kRows ? 64 : 768))) continue;
+        const int high = i8_tile_rows(c.form);
+        const int64_t units = mode == I8Mode::kRows ? std::max(f8_ceil(2 * rows + sought * high, 2 * high), sought) : f8_ceil(a.m, high) * groups;
+        const int64_t tiles = units * f8_ceil(a.n, i8_tile_cols(c.form)), round = 256 * c.share, rounds = tiles / round, rest = f8_ceil(tiles - rounds * round, 256);
+        const double whole = c.per_tile + blocks * (c.first_block + (c.share - 1) * c.further_block);
+        double us = c.once + rounds * whole;
+        if (rest) us += c.per_tile + blocks * (c.first_block + (rest - 1) * c.further_block);
+        // (by rows the number of tiles is an estimate, and what units share of a weight is read more often)
+        if (mode == I8Mode::kRows && rounds == 0 && c.form == I8Form::kMiddle) us *= 1.12;
+        if (mode == I8Mode::kRows && rounds > 0) us = c.once + (c.form == I8Form::kSmall ? 1.35 : c.form == I8Form::kMiddle ? 1.2 : 1.08) * ((double)tiles / round + 0.3) * whole;
+        if (us < least) { least = us; best = c.form; }
+    }
+    return best;
 }
-
 // Workgroups of a launch.
 inline int64_t i8_tiles(I8Mode mode, I8Form form, const I8Args &a) {
     const int64_t tiles_n = f8_ceil(a.n, i8_tile_cols(form));
@@ -157,15 +174,24 @@ inline int64_t i8_quantize_pieces(const I8Groups &g, int64_t each, int64_t parts
 }
 
 // lanes: threads to a row that is held (0: it is read twice); rows_each: rows of a workgroup that converts them and takes the maxima of columns with them, 0: it
-// takes none; columns_each: rows of one that takes maxima of columns only, 0: there is none.
+// takes none; columns_each: rows of one that takes maxima of columns only, 0: there is none; strips: the transpose in one launch, and
+// what is written as it is, too, of up to kI8StripCols columns.
 struct I8ConvertPlan {
     int lanes, rows_each, columns_each;
+    bool strips;
 };
+constexpr int kI8StripCols = 2048;
 inline I8ConvertPlan i8_convert_plan(const I8Quantize &p) {
     const int64_t rows = p.groups.rows, groups = p.groups.groups;
-    I8ConvertPlan plan{p.cols <= 32 ? 4 : p.cols <= 128 ? 16 : p.cols <= 512 ? 64 : p.cols <= kI8MostHeld ? 256 : 0, 0, 0};
+    I8ConvertPlan plan{p.cols <= 32 ? 4 : p.cols <= 128 ? 16 : p.cols <= 512 ? 64 : p.cols <= kI8MostHeld ? 256 : 0, 0, 0, false};
     if (p.cols > 2048 && plan.lanes && rows <= 512) plan.lanes = 1024;
     if (!p.qt) return plan;
+    // Few rows to a group (by group the mean says less): one launch.  Three or four | one, us, both forms: 100 x 100 bf16 10.5 | 4.5, 512 x 4096 15.7 | 13.3, 64 of 128 x 512
+    // 15.5 | 9.4, 1000 x 1000 15.1 | 16.9, 4000 x 64 12.2 | 37.7.
+    if (rows <= (p.groups.offsets ? 384 : 512) * groups && rows * p.cols <= 1 << 22) {
+        plan.strips = true;
+        return plan;
+    }
     // Atomic maxima of one scale take about 20 ns each, one after the other, so at most 128 workgroups raise the same ones (1024 did: 16384 x 512 bf16 22 us, now 7).
     // With the rows (one read less) where that leaves workgroups enough for the device, or little work in all.  Together | apart, us: 8 of 4096 x 2048 f32 126 | 152,
     // 200 x 400 f32 10.1 | 14.0; 4096 x 4096 bf16 50 | 35, 16384 x 4096 150 | 96.
@@ -188,7 +214,8 @@ inline int64_t i8_quantize_threads(const I8Quantize &p) {
         most = plan.rows_each ? i8_quantize_pieces(p.groups, plan.rows_each, 1) * kI8RowThreads
                : plan.lanes   ? f8_ceil(rows * plan.lanes, kI8RowThreads) * kI8RowThreads
                               : rows * 1024;
-    if (p.qt) {
+    if (plan.strips) most = std::max(most, (f8_ceil(p.cols, 32) * p.groups.groups + f8_ceil(rows, 4)) * 256);
+    else if (p.qt) {
         most = std::max(most, f8_ceil(p.side_by_side ? p.cols : p.cols * p.groups.groups, 256) * 256 * (p.side_by_side ? p.groups.groups : 1));
         if (plan.columns_each) most = std::max(most, i8_quantize_pieces(p.groups, plan.columns_each, f8_ceil(p.cols, p.cols <= 32 ? 32 : p.cols <= 128 ? 128 : 512)) * kI8ColumnThreads);
         most = std::max(most, i8_quantize_pieces(p.groups, 128, f8_ceil(p.cols, 128)) * kI8TileThreads);

@@ -54,7 +54,9 @@ __device__ __forceinline__ void quantize(const float (&x)[N], const Scaled (&by)
 #pragma unroll
         for (int u = 0; u < 4; ++u) w[u] = __builtin_bit_cast(uint32_t, t[i + u]);
         const uint32_t lo = __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u);
-        words[i / 4] = by[i / RUN].r > 0.0f ? __builtin_amdgcn_perm(hi, lo, 0x05040100u) : 0u;
+        const uint32_t word = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+        if constexpr (RUN >= 4) words[i / 4] = by[i / RUN].r > 0.0f ? word : 0u;
+        else words[i / 4] = (by[i / RUN].r > 0.0f ? word & 0xffffu : 0u) | (by[i / RUN + 1].r > 0.0f ? word & 0xffff0000u : 0u);
     }
 }
 
@@ -77,7 +79,8 @@ template <int LANES>
 __device__ __forceinline__ float max_over(float magnitude) {
     uint32_t x = __builtin_bit_cast(uint32_t, magnitude) & 0x7fffffffu;
     x = max_moved<0x4e>(max_moved<0xb1>(x));                   // within 4 lanes: [1 0 3 2], [2 3 0 1]
-    if constexpr (LANES >= 16) x = max_moved<0x140>(max_moved<0x141>(x));    // the halves of 8 lanes, then of 16, mirrored
+    if constexpr (LANES >= 8) x = max_moved<0x141>(x);         // the halves of 8 lanes mirrored, then of 16
+    if constexpr (LANES >= 16) x = max_moved<0x140>(x);
     if constexpr (LANES >= 64) {
         const auto q = __builtin_amdgcn_permlane16_swap(x, x, false, false);
         x = max((uint32_t)q[0], (uint32_t)q[1]);
@@ -373,6 +376,128 @@ __global__ __launch_bounds__(kI8TileThreads, 8) void k_i8_turn(I8Quantize p, int
     }
 }
 
+// Everything of a small call in one launch: workgroups from `row_groups` on take 32 columns of a group each, read them for their scales and again for their
+// bytes, 64 rows at a time (a row to 4 threads) and 128 in LDS; those before take 4 rows each as they are, of up to 2048 columns.
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_i8_strips(I8Quantize p, int row_groups, int strips) {
+    __shared__ __align__(16) float tops[256 * 8];
+    if ((int)blockIdx.x < row_groups) {                        // uniform
+        const int lane = threadIdx.x & 63, cols = (int)p.cols;
+        const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+        if (r >= p.groups.rows) return;
+        const int64_t from = source_row(p, r);
+        const typename Eight<TYPE>::T *const row = static_cast<const typename Eight<TYPE>::T *>(p.X) + max(from, (int64_t)0) * p.ldx;
+        Eight<TYPE> in[4];
+        float x[4][8], top = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            if (h * 512 < cols) ask(in[h], row, h * 512 + lane * 8, cols, (h + 1) * 512 <= cols);
+        int64_t lo, hi;
+        rows_written(p, lo, hi);
+        if (r < lo || r >= hi) return;
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            if (h * 512 < cols) {
+                settle(in[h], h * 512 + lane * 8, cols, (h + 1) * 512 <= cols, from < 0);
+                in[h].get(x[h]);
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) top = max_magnitude(top, x[h][i], x[h][i + 1]);
+            }
+        const float s = scale_of(max_over<64>(top));
+        const Scaled by[1] = {Scaled(s)};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int c = h * 512 + lane * 8;
+            if (h * 512 < cols) {
+                uint32_t w[2];
+                quantize(x[h], by, w);
+                if ((c & ~15) < cols) *reinterpret_cast<uint2 *>(p.q + r * p.ld + c) = make_uint2(w[0], w[1]);
+            }
+        }
+        if (lane == 0) p.scale[r] = s;
+        return;
+    }
+    const int id = (int)blockIdx.x - row_groups, g = id / strips, c0 = (id - g * strips) * 32, cols = (int)p.cols, t = (int)threadIdx.x;
+    const int sub = t >> 2, c = c0 + (t & 3) * 8;
+    const bool inside = c0 + 32 <= cols;
+    const I8Span span = i8_span(p.groups, g);
+    const auto row_of = [&](int64_t from) { return static_cast<const typename Eight<TYPE>::T *>(p.X) + max(from, (int64_t)0) * p.ldx; };
+    float top[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top[i] = 0.0f;
+    for (int r = span.lo + sub; r < span.hi; r += 256) {
+        Eight<TYPE> in[4];
+        int64_t from[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) from[u] = source_row(p, min(r + 64 * u, span.hi - 1));  // (a row twice changes no maximum)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) ask(in[u], row_of(from[u]), c, cols, inside);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) settle(in[u], c, cols, inside, from[u] < 0);
+#pragma unroll
+        for (int u = 0; u < 4; u += 2) {
+            float x[8], y[8];
+            in[u].get(x);
+            in[u + 1].get(y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top[i] = max_magnitude(top[i], x[i], y[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) *reinterpret_cast<f8_v4f *>(tops + t * 8 + i) = f8_v4f{top[i], top[i + 1], top[i + 2], top[i + 3]};
+    __syncthreads();
+    {   // 8 threads to a column, 8 rows of threads each
+        float most = 0.0f;
+        const int column = t >> 3;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) most = max_magnitude(most, tops[((t & 7) * 8 + u) * 32 + column], 0.0f);
+        most = max_over<8>(most);
+        const float s = scale_of(most);
+        __syncthreads();
+        if ((t & 7) == 0) {
+            tops[column] = s;
+            if (c0 + column < cols) p.scale_t[(int64_t)g * p.ld_scale_t + c0 + column] = s;
+        }
+    }
+    __syncthreads();
+    const Scaled by[8] = {Scaled(tops[c - c0]), Scaled(tops[c - c0 + 1]), Scaled(tops[c - c0 + 2]), Scaled(tops[c - c0 + 3]),
+                          Scaled(tops[c - c0 + 4]), Scaled(tops[c - c0 + 5]), Scaled(tops[c - c0 + 6]), Scaled(tops[c - c0 + 7])};
+    uint8_t *const turned = reinterpret_cast<uint8_t *>(tops + 64);        // [32 columns][128 rows], chunk r / 16 of column c at place (r / 16) ^ (c % 8)
+    int8_t *const out = p.qt + (p.side_by_side ? i8_first_col(span) : (int64_t)g * p.cols * p.ldt);
+    for (int r0 = span.lo; r0 < span.hi; r0 += 128) {
+        const int rows = min(128, span.hi - r0);
+        Eight<TYPE> in[2];
+        int64_t from[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) from[u] = source_row(p, r0 + min(2 * sub + u, rows - 1));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) ask(in[u], row_of(from[u]), c, cols, inside);
+        float x[2][8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            settle(in[u], c, cols, inside, from[u] < 0 || 2 * sub + u >= rows);
+            in[u].get(x[u]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const float pairs[4] = {x[0][j], x[1][j], x[0][j + 1], x[1][j + 1]};
+            const Scaled two[2] = {by[j], by[j + 1]};
+            uint32_t w[1];
+            quantize(pairs, two, w);
+            const int col = c - c0 + j;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                *reinterpret_cast<uint16_t *>(turned + (col + u) * 128 + (sub >> 3 ^ (col + u & 7)) * 16 + (sub & 7) * 2) = (uint16_t)(w[0] >> 16 * u);
+        }
+        __syncthreads();
+        const int row = t >> 3, chunk = t & 7;
+        if (c0 + row < cols && (p.side_by_side || chunk * 16 < rows))
+            *reinterpret_cast<f8_v4i *>(out + (int64_t)(c0 + row) * p.ldt + (r0 - span.lo) + chunk * 16) =
+                *reinterpret_cast<const f8_v4i *>(turned + row * 128 + (chunk ^ (row & 7)) * 16);
+        __syncthreads();
+    }
+}
+
 template <int TYPE, int HELD, int LANES, int THREADS = kI8RowThreads>
 hipError_t launch_rows(const I8Quantize &p, int each, hipStream_t stream) {
     if constexpr (THREADS == kI8RowThreads) {
@@ -395,7 +520,12 @@ template <int TYPE>
 hipError_t launch(const I8Quantize &p, hipStream_t stream) {
     const int64_t cols = p.cols;
     const I8ConvertPlan plan = i8_convert_plan(p);
-    if (p.qt) {
+    if (plan.strips) {
+        const int64_t strips = f8_ceil(cols, 32), row_groups = p.q && cols <= kI8StripCols ? f8_ceil(p.groups.rows, 4) : 0;
+        hipLaunchKernelGGL((k_i8_strips<TYPE>), dim3((unsigned)(row_groups + strips * p.groups.groups)), dim3(256), 0, stream, p, (int)row_groups, (int)strips);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (!p.q || row_groups) return hipSuccess;
+    } else if (p.qt) {
         const int64_t run = p.side_by_side ? cols : p.groups.groups * cols;      // of scales without a gap
         hipLaunchKernelGGL(k_i8_least_scales, dim3((unsigned)f8_ceil(run, 256), p.side_by_side ? (unsigned)p.groups.groups : 1u), dim3(256), 0, stream, p.scale_t,
                            p.ld_scale_t, (int)run);
@@ -421,7 +551,7 @@ hipError_t launch(const I8Quantize &p, hipStream_t stream) {
         }
         if (e) return e;
     }
-    if (!p.qt) return hipSuccess;
+    if (!p.qt || plan.strips) return hipSuccess;
     if (plan.columns_each) {
         const int each = plan.columns_each;
         if (hipError_t e = cols <= 32 ? launch_columns<TYPE, 4>(p, each, stream) : cols <= 128 ? launch_columns<TYPE, 16>(p, each, stream)

@@ -103,7 +103,7 @@ hipError_t launch_rows(const I8Args &args, int rows, hipStream_t stream) {
 
 hipError_t launch_i8_thin(I8Mode mode, const I8Args &args, hipStream_t stream) {
     return mode == I8Mode::kDense ? launch_rows<I8Mode::kDense>(args, args.m, stream)
-                                  : launch_rows<I8Mode::kRows>(args, 2 * (args.groups.rows / args.groups.groups), stream);
+                                  : launch<1, I8Mode::kRows>(args, stream);
 }
 
 }  // namespace oz2

@@ -37,6 +37,7 @@ struct I8Args {
     I8Groups groups;
     int ranges, kb_each;                   // kDense: K ranges and their length in blocks
     int only_short;                        // kSums: groups that large tiles take have been served
+    int turn;                              // large tiles of a round (one to a compute unit); kDense, kRows: if a last round is short, tiles of kMiddle take its place
     F8Out out;                             // (planes hold int32 sums)
 };
 
@@ -70,6 +71,12 @@ constexpr int kI8WideBlocks = 3;           // what the kernel of large tiles nee
 constexpr int kI8WideGroups = 1024;        // and the most groups that it keeps in LDS
 // kSums: groups that it takes; the other ones are left to small tiles.
 OZ2_HOST_DEVICE inline bool i8_by_large_tiles(int rows) { return rows > (kI8WideBlocks - 1) * kI8Block && rows <= kI8MaxK; }
+// Of `share` large tiles, `turn` of which go at a time, those that are left to tiles of 64 x 128 (8 for a large one): the ones of a last round, not the only one, that has at
+// most 3 / 8 of its places filled.  kRows counts by XCD.  16384 x 2048 x 4096 in 8 groups of 500 to 4000 rows, 560 tiles: 148 -> 122 us; one group, 512 tiles, 110.
+OZ2_HOST_DEVICE inline uint32_t i8_left_over(uint32_t share, uint32_t turn) {
+    const uint32_t rest = share % turn;
+    return share > turn && rest <= turn * 3 / 8 ? rest : 0;
+}
 // Whether large tiles can serve a call at all.
 inline bool i8_large_possible(I8Mode mode, const I8Args &a) {
     return a.m >= 256 && a.n >= 256 && (mode == I8Mode::kDense || a.groups.groups <= kI8WideGroups) && (mode == I8Mode::kSums || i8_blocks(a.k) >= kI8WideBlocks);
@@ -117,7 +124,9 @@ inline I8Plan i8_plan(int64_t m, int64_t n, int64_t k) {
             const int64_t items = tiles * ranges, rounds = items / round, rest = f8_ceil(items - rounds * round, 256);
             const size_t planes = ranges == 1 ? 0 : (size_t)ranges * (size_t)m * (size_t)i8_plane_ld(n) * 4;
             double us = c.once + rounds * (c.per_tile + each * (c.first_block + (c.share - 1) * c.further_block));
-            if (rest) us += c.per_tile + each * (c.first_block + (rest - 1) * c.further_block);
+            if (c.form == I8Form::kLarge && ranges == 1 && i8_left_over((uint32_t)tiles, 256))
+                us += 3.0 + f8_ceil((items - rounds * round) * 8, 512) * (kI8Costs[1].per_tile + each * (kI8Costs[1].first_block + kI8Costs[1].further_block));
+            else if (rest) us += c.per_tile + each * (c.first_block + (rest - 1) * c.further_block);
             us = std::max(us, 3.0 + (double)(m + n) * k / kI8BytesPerUs) + (planes ? kI8RangesOnce + planes / kI8PlaneBytesPerUs : 0.0);
             if (us < best.us) best = I8Plan{c.form, (int)ranges, (int)each, planes, us};
         }
@@ -226,6 +235,7 @@ inline int64_t i8_quantize_threads(const I8Quantize &p) {
 #if defined(__HIPCC__)
 hipError_t launch_i8_thin(I8Mode mode, const I8Args &args, hipStream_t stream);
 hipError_t launch_i8_wide(I8Mode mode, const I8Args &args, hipStream_t stream);
+hipError_t i8_units(int *units);              // compute units of the current device, in whole rounds of the XCDs
 hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream);
 hipError_t launch_i8_quantize(const I8Quantize &args, int type, hipStream_t stream);
 #endif

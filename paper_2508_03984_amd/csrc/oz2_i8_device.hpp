@@ -28,18 +28,18 @@ __device__ __forceinline__ uint32_t i8_running_sum(uint32_t x) {
 }
 __device__ __forceinline__ uint32_t i8_last(uint32_t running) { return (uint32_t)__builtin_amdgcn_readlane((int)running, 63); }
 
-// The groups cut into units of `each` rows, `per` pieces of work to a unit.  A workgroup's place among them, from its id: each of the 8 XCDs, to which ids go in
-// turns, has neighbouring pieces of one group, which share their operands in its L2.  False if there is none for the id.  A wavefront does this together, 64 groups
-// at a time; piece counts of offsets that do not ascend may be anything, but a span is always one of i8_span's.
+// The groups cut into units of `each` rows, `per` pieces of work to a unit: the piece at the place that `choose` gives for their number (none: -1); false if there is
+// none.  A wavefront does this together, 64 groups at a time; piece counts of offsets that do not ascend may be anything, but a span is always one of i8_span's.
 struct I8Place {
     I8Span span;
     uint32_t units, piece;                                     // of the group; 0 .. units * per - 1
 };
-__device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t per, uint32_t id, I8Place &out) {
+template <typename Choose>
+__device__ __forceinline__ bool i8_find_place(const I8Groups &s, int each, uint32_t per, Choose &&choose, I8Place &out) {
     if (!s.offsets) {
         out.units = (uint32_t)(s.each + each - 1) / (uint32_t)each;
-        const uint32_t pieces = out.units * per, total = pieces * (uint32_t)s.groups, share = (total + 7) / 8, place = (id & 7) * share + (id >> 3);
-        if ((id >> 3) >= share || place >= total) return false;
+        const uint32_t pieces = out.units * per, place = choose(pieces * (uint32_t)s.groups);
+        if (place >= pieces * (uint32_t)s.groups) return false;
         const int g = (int)(place / pieces);
         out.span = i8_span(s, g);
         out.piece = place - (uint32_t)g * pieces;
@@ -51,12 +51,11 @@ __device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t pe
         const I8Span span = i8_span(s, g);
         return (uint32_t)(span.hi - span.lo + each - 1) / (uint32_t)each;
     };
-    uint32_t total = 0, first = count(lane), running = i8_running_sum(first);
-    total = i8_last(running);
+    uint32_t first = count(lane), running = i8_running_sum(first), total = i8_last(running);
     for (int g0 = 64; g0 < s.groups; g0 += 64) total += i8_last(i8_running_sum(count(g0 + lane)));
     total *= per;
-    const uint32_t share = (total + 7) / 8, place = (id & 7) * share + (id >> 3);
-    if ((id >> 3) >= share || place >= total) return false;    // uniform
+    const uint32_t place = choose(total);
+    if (place >= total) return false;                          // uniform
     const uint32_t unit = place / per;
     uint32_t before = 0;
     for (int g0 = 0; g0 < s.groups; g0 += 64) {
@@ -79,6 +78,13 @@ __device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t pe
         before += i8_last(running);
     }
     return false;
+}
+// A workgroup's piece, from its id: each of the 8 XCDs, to which ids go in turns, has neighbouring pieces, which share their operands in its L2.
+__device__ __forceinline__ bool i8_find(const I8Groups &s, int each, uint32_t per, uint32_t id, I8Place &out) {
+    return i8_find_place(s, each, per, [&](uint32_t total) {
+        const uint32_t share = (total + 7) / 8;
+        return (id >> 3) < share ? (id & 7) * share + (id >> 3) : ~0u;
+    }, out);
 }
 
 // First column of a group whose rows lie side by side with the others'.

@@ -56,17 +56,26 @@ __device__ __forceinline__ void place_in_group(uint32_t piece, uint32_t units, u
     tr = (int)(band * 8 + left - (uint32_t)tc * high);
 }
 
-template <I8Mode MODE, int BM, int BN>
+// LAST: of the large tiles that the launch before has left, BM x BN parts; the map is that of the large tiles.
+template <I8Mode MODE, int BM, int BN, bool LAST>
 __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, int id, Tile &t) {
+    constexpr int HIGH = LAST ? 256 : BM, BROAD = LAST ? 256 : BN, PARTS = HIGH * BROAD / (BM * BN), ACROSS = BROAD / BN;
     t.lost = false;
     t.range = 0;
     if constexpr (MODE == I8Mode::kRows) {
-        const uint32_t tiles_n = (uint32_t)(p.n + BN - 1) / BN;
+        const uint32_t tiles_n = (uint32_t)(p.n + BROAD - 1) / BROAD;
         I8Place at;
-        if (!i8_find(p.groups, BM, tiles_n, (uint32_t)id, at)) return false;
+        if constexpr (LAST) {
+            const bool found = i8_find_place(p.groups, HIGH, tiles_n, [&](uint32_t total) {
+                const uint32_t share = (total + 7) / 8, left = i8_left_over(share, (uint32_t)p.turn / 8), local = (uint32_t)(id >> 3) / PARTS;
+                return local < left ? (uint32_t)(id & 7) * share + share - left + local : ~0u;
+            }, at);
+            if (!found) return false;
+        } else if (!i8_find(p.groups, HIGH, tiles_n, (uint32_t)id, at)) return false;
         int tr, tc;
         place_in_group(at.piece, at.units, tiles_n, tr, tc);
-        const int row0 = at.span.lo + tr * BM, col0 = tc * BN;
+        const int part = LAST ? (id >> 3) % PARTS : 0, row0 = at.span.lo + tr * HIGH + part / ACROSS * BM, col0 = tc * BROAD + part % ACROSS * BN;
+        if (LAST && (row0 >= at.span.hi || col0 >= p.n)) return false;
         const int64_t b_row = (int64_t)at.span.group * p.n + col0;
         t.rows = min(BM, at.span.hi - row0);
         t.cols = min(BN, p.n - col0);
@@ -81,8 +90,10 @@ __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, i
         t.c_col = col0;
     } else {
         int s, tr, tc;
-        map_tile(map, id, s, tr, tc);
-        const int row0 = tr * BM, col0 = tc * BN;
+        const int first_left = LAST ? map.total - (int)i8_left_over((uint32_t)map.total, (uint32_t)p.turn) : 0, part = LAST ? id % PARTS : 0;
+        map_tile(map, LAST ? first_left + id / PARTS : id, s, tr, tc);
+        const int row0 = tr * HIGH + part / ACROSS * BM, col0 = tc * BROAD + part % ACROSS * BN;
+        if (LAST && (row0 >= p.m || col0 >= p.n)) return false;
         t.rows = min(BM, p.m - row0);
         t.cols = min(BN, p.n - col0);
         t.c_col = col0;
@@ -114,13 +125,13 @@ __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, i
     return true;
 }
 
-template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE>
+template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE, bool LAST>
 __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, TileMap map) {
     typedef I8Core<WM, WN, FM, FN, STAGES> C;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN, lrow = lane & 15, quarter = lane >> 4;
     Tile t;
-    if (!find_tile<MODE, C::BM, C::BN>(p, map, (int)blockIdx.x, t)) return;
+    if (!find_tile<MODE, C::BM, C::BN, LAST>(p, map, (int)blockIdx.x, t)) return;
     const int KB = (t.k + kI8Block - 1) / kI8Block, kb0 = t.kb0, kb1 = t.kb1;
 
     const bool none = kb0 >= kb1;
@@ -282,20 +293,24 @@ __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, Ti
     }
 }
 
-template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE>
+template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE, bool LAST = false>
 hipError_t launch_tiles(const I8Args &args, I8Form form, hipStream_t stream) {
     typedef I8Core<WM, WN, FM, FN, STAGES> C;
     static thread_local int attr_device = -1;                // the attribute is per device (set again per thread: harmless)
     int dev = -1;
     if (hipError_t e = hipGetDevice(&dev)) return e;
     if (attr_device != dev) {
-        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_i8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, MODE>),
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_i8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, MODE, LAST>),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS_BYTES)) return e;
         attr_device = dev;
     }
-    const int64_t tiles = i8_tiles(MODE, form, args);
-    const TileMap map = MODE == I8Mode::kRows ? TileMap{} : make_tile_map((args.m + C::BM - 1) / C::BM, (args.n + C::BN - 1) / C::BN, (int)tiles);
-    hipLaunchKernelGGL((k_i8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, MODE>), dim3((unsigned)tiles), dim3(C::THREADS), C::LDS_BYTES, stream, args, map);
+    constexpr int HIGH = LAST ? 256 : C::BM, BROAD = LAST ? 256 : C::BN;
+    const int64_t all = i8_tiles(MODE, LAST ? I8Form::kLarge : form, args);
+    // (kRows: as many as a last round that is left may have)
+    const int64_t tiles = !LAST ? all : (MODE == I8Mode::kDense ? (int64_t)i8_left_over((uint32_t)all, (uint32_t)args.turn) : std::min<int64_t>(args.turn * 3 / 8, all)) * (256 * 256 / (C::BM * C::BN));
+    if (tiles == 0) return hipSuccess;
+    const TileMap map = MODE == I8Mode::kRows ? TileMap{} : make_tile_map((args.m + HIGH - 1) / HIGH, (args.n + BROAD - 1) / BROAD, (int)all);
+    hipLaunchKernelGGL((k_i8_tiles<WM, WN, FM, FN, STAGES, PER_SIMD, MODE, LAST>), dim3((unsigned)tiles), dim3(C::THREADS), C::LDS_BYTES, stream, args, map);
     return hipGetLastError();
 }
 
@@ -328,6 +343,9 @@ hipError_t launch_form(const I8Args &args, I8Form form, hipStream_t stream) {
                        : tiles <= 512            ? launch_tiles<2, 2, 2, 2, 4, 2, MODE>(args, form, stream)
                        : tiles <= 768            ? launch_tiles<2, 2, 2, 2, 3, 3, MODE>(args, form, stream)
                                                  : launch_tiles<2, 2, 2, 2, 2, 4, MODE>(args, form, stream)) return e;
+    if constexpr (MODE != I8Mode::kSums) {
+        if (form == I8Form::kLarge && args.ranges <= 1) return launch_tiles<2, 2, 2, 4, 3, 2, MODE, true>(args, I8Form::kMiddle, stream);
+    }
     if (MODE != I8Mode::kDense || args.ranges <= 1) return hipSuccess;
     const int64_t threads = (int64_t)args.m * ((args.n + 3) / 4);
     hipLaunchKernelGGL(k_i8_ranges, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, args);
@@ -338,6 +356,9 @@ hipError_t launch_form(const I8Args &args, I8Form form, hipStream_t stream) {
 
 hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream) {
     if (form == I8Form::kThin) return launch_i8_thin(mode, args, stream);
+    if (form == I8Form::kLarge) {
+        if (hipError_t e = i8_units(&args.turn)) return e;
+    }
     if (form == I8Form::kLarge && mode == I8Mode::kSums) {
         if (hipError_t e = launch_i8_wide(mode, args, stream)) return e;
         args.only_short = 1;

@@ -61,6 +61,7 @@ __device__ __forceinline__ int accumulator() {
 struct WideArgs {
     I8Args p;
     TileMap map;
+    int end;                                                  // kDense, kSums: tiles that are taken
     int tiles_n;                                              // kRows: of a group's
     Divisor by_row, by_band;                                  // by that, and by 8 times that
 };
@@ -175,7 +176,7 @@ struct Wide {
         const ArgsPtr a = arguments();
         if constexpr (MODE == I8Mode::kRows) {
             const uint32_t share = (total + 7) / 8, place = (uint32_t)(id & 7) * share + (uint32_t)(id >> 3);
-            if ((uint32_t)(id >> 3) >= share || place >= total) return false;
+            if ((uint32_t)(id >> 3) >= share - i8_left_over(share, (uint32_t)a->p.turn / 8) || place >= total) return false;
             const uint32_t tiles_n = (uint32_t)a->tiles_n, unit = (uint32_t)divide((int)place, a->by_row.mul, a->by_row.shift);
             const int groups = a->p.groups.groups;
             for (int g0 = 0; g0 < groups; g0 += 64) {
@@ -196,7 +197,7 @@ struct Wide {
             }
             return false;
         } else {
-            if (id >= a->map.total) return false;
+            if (id >= a->end) return false;
             int which, tr, tc;
             map_tile_at(&a->map, id, which, tr, tc);
             it.which = uniform(which);
@@ -213,7 +214,7 @@ struct Wide {
     // The next id from `id` on, in steps of the grid, that has work.
     __device__ __forceinline__ bool find_from(int &id, Item &it) const {
         if constexpr (MODE == I8Mode::kSums) {
-            const int end = arguments()->map.total;
+            const int end = arguments()->end;
             for (; id < end; id += (int)gridDim.x)
                 if (find(id, it)) return true;
             return false;
@@ -583,22 +584,34 @@ hipError_t launch(const I8Args &args, hipStream_t stream) {
     static thread_local int attr_device = -1;                // the attribute is per device (set again per thread: harmless)
     int dev = -1;
     if (hipError_t e = hipGetDevice(&dev)) return e;
-    static thread_local int units = 0;                       // compute units of that device, in whole rounds of the XCDs
     if (attr_device != dev) {
         if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_i8_wide<MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kWideLdsBytes)) return e;
-        if (hipError_t e = hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, dev)) return e;
-        units = std::max(units / 8 * 8, 8);
         attr_device = dev;
     }
     const int tiles_n = (args.n + 255) / 256;
     const int64_t tiles = i8_tiles(MODE, I8Form::kLarge, args);
     const TileMap map = MODE == I8Mode::kRows ? TileMap{} : make_tile_map((args.m + 255) / 256, tiles_n, (int)tiles);
-    hipLaunchKernelGGL(k_i8_wide<MODE>, dim3((unsigned)std::min<int64_t>(tiles, units)), dim3(256), kWideLdsBytes, stream,
-                       WideArgs{args, map, tiles_n, make_divisor(tiles_n), make_divisor(8 * tiles_n)});
+    const int end = (int)tiles - (MODE == I8Mode::kDense && args.ranges == 1 ? (int)i8_left_over((uint32_t)tiles, (uint32_t)args.turn) : 0);
+    if (end == 0) return hipSuccess;
+    hipLaunchKernelGGL(k_i8_wide<MODE>, dim3((unsigned)std::min<int64_t>(MODE == I8Mode::kRows ? tiles : end, args.turn)), dim3(256), kWideLdsBytes, stream,
+                       WideArgs{args, map, end, tiles_n, make_divisor(tiles_n), make_divisor(8 * tiles_n)});
     return hipGetLastError();
 }
 
 }  // namespace
+
+hipError_t i8_units(int *units) {
+    static thread_local int device = -1, found = 0;
+    int dev = -1;
+    if (hipError_t e = hipGetDevice(&dev)) return e;
+    if (device != dev) {
+        if (hipError_t e = hipDeviceGetAttribute(&found, hipDeviceAttributeMultiprocessorCount, dev)) return e;
+        found = std::max(found / 8 * 8, 8);
+        device = dev;
+    }
+    *units = found;
+    return hipSuccess;
+}
 
 hipError_t launch_i8_wide(I8Mode mode, const I8Args &args, hipStream_t stream) {
     return mode == I8Mode::kDense ? launch<I8Mode::kDense>(args, stream) : mode == I8Mode::kRows ? launch<I8Mode::kRows>(args, stream) : launch<I8Mode::kSums>(args, stream);

@@ -17,7 +17,7 @@ def f32(x):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m,n,k", [(2048, 2048, 384), (2049, 2305, 385), (4095, 1030, 1000), (2300, 2060, 513), (1111, 4099, 640), (2048, 2050, 2047), (9000, 300, 500),
-                                   (257, 16400, 700)])
+                                   (257, 16400, 700), (4300, 4400, 400), (4097, 4097, 515)])
 def test_product(m, n, k, dtype):
     g = gen(m + n + k)
     a, b = operand(g, m, k), operand(g, n, k)
@@ -45,7 +45,7 @@ LONG = [[0, 256, 512, 2048], [5, 300, 301, 301, 1400, 2000, 2900], [0, 1, 2, 3, 
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("offsets", LONG, ids=lambda o: f"{len(o) - 1}_groups_{o[-1]}")
-@pytest.mark.parametrize("n,k", [(2048, 384), (1111, 1000), (2300, 513)])
+@pytest.mark.parametrize("n,k", [(2048, 384), (1111, 1000), (2300, 513), (5000, 640), (7000, 400)])
 def test_grouped(offsets, n, k, dtype):
     rows, groups, g = offsets[-1] + 7, len(offsets) - 1, gen(n + k)
     a, b = operand(g, rows, k), operand(g, groups * n, k)

@@ -11,13 +11,16 @@ from test_gpu_i8 import TYPES, gen, operand, output, outside_kept
 pytestmark = pytest.mark.gpu
 
 
+PRODUCTS = [(2048, 2048, 384), (2049, 2305, 385), (4095, 1030, 1000), (2300, 2060, 513), (1111, 4099, 640), (2048, 2050, 2047), (9000, 300, 500), (257, 16400, 700),
+            (4300, 4400, 400), (4097, 4097, 515), (2048, 2048, 2048), (1024, 4099, 3333), (1536, 1000, 40000), (1537, 1001, 39999), (3000, 3100, 3001), (3841, 4093, 1920)]
+
+
 def f32(x):
     return torch.tensor(x).double().item()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m,n,k", [(2048, 2048, 384), (2049, 2305, 385), (4095, 1030, 1000), (2300, 2060, 513), (1111, 4099, 640), (2048, 2050, 2047), (9000, 300, 500),
-                                   (257, 16400, 700), (4300, 4400, 400), (4097, 4097, 515)])
+@pytest.mark.parametrize("m,n,k", PRODUCTS)
 def test_product(m, n, k, dtype):
     g = gen(m + n + k)
     a, b = operand(g, m, k), operand(g, n, k)
@@ -67,9 +70,12 @@ def test_grouped(offsets, n, k, dtype):
         outside_kept(c, buf, before)
 
 
+SUMS = [(o, m, n) for o in LONG for m, n in ((1024, 2048), (1111, 1300), (257, 5000))]
+SUMS += [([0, 100, 3000, 3256, 6000], 2304, 4099), ([7, 7, 5000, 5001, 9000], 2305, 2305), ([0, 257, 514, 4000, 4000, 4004], 4097, 2305), ([3, 2000, 2048], 4100, 4100)]
+
+
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("offsets", LONG, ids=lambda o: f"{len(o) - 1}_groups_{o[-1]}")
-@pytest.mark.parametrize("m,n", [(1024, 2048), (1111, 1300), (257, 5000)])
+@pytest.mark.parametrize("offsets,m,n", SUMS, ids=lambda o: f"{len(o) - 1}_groups_{o[-1]}" if isinstance(o, list) else str(o))
 def test_grouped_grad(offsets, m, n, dtype):
     rows, groups, g = offsets[-1] + 7, len(offsets) - 1, gen(n + m)
     off = torch.tensor(offsets, dtype=torch.int32, device="cuda")

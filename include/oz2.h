@@ -32,8 +32,8 @@
  *     launches anything;
  *   - inputs must be finite.  Inf/NaN inputs give an unspecified (but memory
  *     safe) result: the paper does not define them;
- *   - no entry point throws; besides the workspace growth above (and hipMalloc for the planes of 8-bit
- *     floating-point products, see oz2_f8_workspace_bytes) only oz2_destroy, oz2_release,
+ *   - no entry point throws; besides the workspace growth above (and hipMalloc for the planes of products
+ *     in 8 bits, see oz2_f8_workspace_bytes) only oz2_destroy, oz2_release,
  *     oz2_set_workspace and oz2_last_stage_times_ms (and their oz2_ctx_ forms) synchronise the device.
  */
 #ifndef OZ2_H
@@ -447,6 +447,8 @@ oz2_status oz2_ctx_i8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, fl
  */
 oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
                                const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream);
+oz2_status oz2_ctx_i8_grouped_gemm(oz2_context *ctx, int64_t rows, int64_t n, int64_t k, int64_t groups, const int32_t *offsets, float alpha,
+                                   const oz2_i8 *A, const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream);
 
 /*
  * The gradients of the weights: C is groups * m x n, and C_g <- alpha * A_g * B_g^T + beta * C_g over the columns of group g of A (m x
@@ -456,8 +458,15 @@ oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t group
 oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
                                const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream);
 
-/* Workspace of oz2_i8_gemm, as for oz2_f8_workspace_bytes, with which it shares its memory. */
+oz2_status oz2_ctx_i8_grouped_grad(oz2_context *ctx, int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha,
+                                   const oz2_i8 *A, const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream);
+
+/*
+ * Workspace of oz2_i8_gemm, of oz2_i8_grouped_gemm (grad = 0) and of oz2_i8_grouped_grad (grad != 0, k = its m): planes for K ranges, as described at
+ * oz2_f8_workspace_bytes, with whose memory they are one.  (Integer sums do not depend on the ranges: without room for planes the results are the same, later.)
+ */
 size_t oz2_i8_workspace_bytes(int64_t m, int64_t n, int64_t k);
+size_t oz2_i8_grouped_workspace_bytes(int64_t rows, int64_t n, int64_t k, int64_t groups, int grad);
 
 /*
  * Constants of Section 4.1 for `num_moduli` moduli, written to HOST arrays of

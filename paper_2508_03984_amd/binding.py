@@ -33,7 +33,7 @@ EXPORTS = [
     "oz2_f8_quantize", "oz2_f8_gemm", "oz2_f8_gated", "oz2_f8_gated_grad", "oz2_f8_workspace_bytes",
     "oz2_ctx_f8_gemm", "oz2_ctx_f8_gated",
     "oz2_i8_quantize", "oz2_i8_quantize_grouped", "oz2_i8_grouped_cols", "oz2_i8_gemm", "oz2_ctx_i8_gemm", "oz2_i8_grouped_gemm", "oz2_i8_grouped_grad",
-    "oz2_i8_workspace_bytes",
+    "oz2_ctx_i8_grouped_gemm", "oz2_ctx_i8_grouped_grad", "oz2_i8_workspace_bytes", "oz2_i8_grouped_workspace_bytes",
 ]
 
 OZ2_OPT_INT32_PRODUCTS, OZ2_OPT_OVERLAP, OZ2_OPT_SMALL_CONVERSION, OZ2_OPT_PROFILING, OZ2_OPT_CUT_LAUNCHES = range(5)
@@ -161,6 +161,9 @@ def load():
     lib.oz2_ctx_i8_gemm.argtypes = [vp] + lib.oz2_i8_gemm.argtypes
     lib.oz2_i8_grouped_gemm.argtypes = [i64, i64, i64, i64, vp, flt, i8, i8, flt, vp, i64, ci, vp]
     lib.oz2_i8_grouped_grad.argtypes = lib.oz2_i8_grouped_gemm.argtypes
+    lib.oz2_ctx_i8_grouped_gemm.argtypes = lib.oz2_ctx_i8_grouped_grad.argtypes = [vp] + lib.oz2_i8_grouped_gemm.argtypes
+    lib.oz2_i8_grouped_workspace_bytes.argtypes = [i64, i64, i64, i64, ci]
+    lib.oz2_i8_grouped_workspace_bytes.restype = C.c_size_t
     lib.oz2_i8_workspace_bytes.argtypes = [i64, i64, i64]
     lib.oz2_i8_workspace_bytes.restype = C.c_size_t
     for name in EXPORTS:
@@ -818,15 +821,37 @@ def oz2_i8_gemm(m, n, k, alpha, A, B, beta, C_, ldc, stream=None) -> None:
            "oz2_i8_gemm")
 
 
+def _grouped_args(rows, n, k, groups, offsets, alpha, A, B, beta, C_, ldc, stream):
+    return (rows, n, k, groups, _int32(offsets, groups + 1), alpha, _i8_ref(A, rows, k), _i8_ref(B, groups * n, k), beta, _dev(C_), ldc, _f8_type(C_),
+            _stream(stream))
+
+
+def oz2_ctx_i8_grouped_gemm(ctx, rows, n, k, groups, offsets, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    _check(load().oz2_ctx_i8_grouped_gemm(_ctx(ctx), *_grouped_args(rows, n, k, groups, offsets, alpha, A, B, beta, C_, ldc, stream)),
+           "oz2_ctx_i8_grouped_gemm")
+
+
 def oz2_i8_grouped_gemm(rows, n, k, groups, offsets, alpha, A, B, beta, C_, ldc, stream=None) -> None:
-    _check(load().oz2_i8_grouped_gemm(rows, n, k, groups, _int32(offsets, groups + 1), alpha, _i8_ref(A, rows, k), _i8_ref(B, groups * n, k), beta,
-                                      _dev(C_), ldc, _f8_type(C_), _stream(stream)), "oz2_i8_grouped_gemm")
+    _check(load().oz2_i8_grouped_gemm(*_grouped_args(rows, n, k, groups, offsets, alpha, A, B, beta, C_, ldc, stream)), "oz2_i8_grouped_gemm")
+
+
+def _grad_args(m, n, rows, groups, offsets, alpha, A, B, beta, C_, ldc, stream):
+    wide = oz2_i8_grouped_cols(rows, groups) if rows else 0
+    return (m, n, rows, groups, _int32(offsets, groups + 1), alpha, _i8_ref(A, m, wide, groups), _i8_ref(B, n, wide, groups), beta, _dev(C_), ldc,
+            _f8_type(C_), _stream(stream))
+
+
+def oz2_ctx_i8_grouped_grad(ctx, m, n, rows, groups, offsets, alpha, A, B, beta, C_, ldc, stream=None) -> None:
+    _check(load().oz2_ctx_i8_grouped_grad(_ctx(ctx), *_grad_args(m, n, rows, groups, offsets, alpha, A, B, beta, C_, ldc, stream)),
+           "oz2_ctx_i8_grouped_grad")
 
 
 def oz2_i8_grouped_grad(m, n, rows, groups, offsets, alpha, A, B, beta, C_, ldc, stream=None) -> None:
-    wide = oz2_i8_grouped_cols(rows, groups) if rows else 0
-    _check(load().oz2_i8_grouped_grad(m, n, rows, groups, _int32(offsets, groups + 1), alpha, _i8_ref(A, m, wide, groups), _i8_ref(B, n, wide, groups),
-                                      beta, _dev(C_), ldc, _f8_type(C_), _stream(stream)), "oz2_i8_grouped_grad")
+    _check(load().oz2_i8_grouped_grad(*_grad_args(m, n, rows, groups, offsets, alpha, A, B, beta, C_, ldc, stream)), "oz2_i8_grouped_grad")
+
+
+def oz2_i8_grouped_workspace_bytes(rows, n, k, groups, grad=False) -> int:
+    return int(load().oz2_i8_grouped_workspace_bytes(rows, n, k, groups, int(bool(grad))))
 
 
 def oz2_i8_workspace_bytes(m, n, k) -> int:

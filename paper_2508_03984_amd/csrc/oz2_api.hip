@@ -1189,9 +1189,27 @@ oz2_status i8_convert(I8Quantize &p, const oz2_i8 *as_is, const oz2_i8 *transpos
     return OZ2_OK;
 }
 
-oz2_status i8_launch(I8Mode mode, const I8Args &args, I8Form form, hipStream_t stream) {
-    if (i8_tiles(mode, mode == I8Mode::kSums ? I8Form::kSmall : form, args) * (form == I8Form::kThin ? 512 : 256) >= kMaxThreads) return OZ2_UNSUPPORTED;
-    OZ2_TRY(launch_i8_product(mode, args, form, stream));
+I8Plan i8_plan_of(I8Mode mode, const I8Args &args, bool one_range) {
+    if (mode == I8Mode::kDense) return one_range ? i8_plan_one_range(args.m, args.n, args.k) : i8_plan(args.m, args.n, args.k);
+    return one_range ? i8_grouped_plan_one_range(mode, args) : i8_grouped_plan(mode, args);
+}
+
+oz2_status i8_run(Ctx &g, I8Mode mode, I8Args &args, hipStream_t stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    I8Plan plan = i8_plan_of(mode, args, false);
+    args.ranges = plan.ranges;
+    const I8Form most = mode == I8Mode::kSums ? I8Form::kSmall : plan.form;    // (short groups are left to smaller tiles)
+    if (i8_tiles(mode, most, args) * 512 >= kMaxThreads) return OZ2_UNSUPPORTED;
+    if (plan.ranges > 1) {
+        if (oz2_status st = f8_planes(g, plan.plane_bytes, &args.out.planes)) return st;
+        if (args.out.planes) {
+            args.out.ldp = i8_plane_ld(args.n);
+            args.out.plane = (int64_t)args.m * (mode == I8Mode::kSums ? args.groups.groups : 1) * args.out.ldp;
+        } else plan = i8_plan_of(mode, args, true);
+    }
+    args.ranges = plan.ranges;
+    args.kb_each = plan.kb_each;
+    OZ2_TRY(launch_i8_product(mode, args, plan.form, stream));
     return OZ2_OK;
 }
 
@@ -1242,21 +1260,7 @@ oz2_status oz2_ctx_i8_gemm(oz2_context *ctx, int64_t m, int64_t n, int64_t k, fl
     if (m > kF8MaxRows || n > kF8MaxRows || k > kI8MaxK) return OZ2_UNSUPPORTED;
     args.m = (int)m; args.n = (int)n; args.k = (int)k;
     args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
-    Ctx &g = resolve(ctx);
-    std::lock_guard<std::mutex> lock(g.mu);
-    I8Plan plan = i8_plan(m, n, k);
-    args.ranges = plan.ranges;
-    if (i8_tiles(I8Mode::kDense, plan.form, args) * 512 >= kMaxThreads) return OZ2_UNSUPPORTED;
-    if (plan.ranges > 1) {
-        if (oz2_status st = f8_planes(g, plan.plane_bytes, &args.out.planes)) return st;
-        if (args.out.planes) {
-            args.out.ldp = i8_plane_ld(n);
-            args.out.plane = m * args.out.ldp;
-        } else plan = i8_plan_one_range(m, n, k);
-    }
-    args.ranges = plan.ranges;
-    args.kb_each = plan.kb_each;
-    return i8_launch(I8Mode::kDense, args, plan.form, stream);
+    return i8_run(resolve(ctx), I8Mode::kDense, args, stream);
 }
 
 oz2_status oz2_i8_gemm(int64_t m, int64_t n, int64_t k, float alpha, const oz2_i8 *A, const oz2_i8 *B, float beta, void *C, int64_t ldc,
@@ -1264,8 +1268,8 @@ oz2_status oz2_i8_gemm(int64_t m, int64_t n, int64_t k, float alpha, const oz2_i
     return oz2_ctx_i8_gemm(nullptr, m, n, k, alpha, A, B, beta, C, ldc, type, stream);
 }
 
-oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
-                               const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
+oz2_status oz2_ctx_i8_grouped_gemm(oz2_context *ctx, int64_t rows, int64_t n, int64_t k, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+                                   const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
     if (rows < 0 || n < 0 || k < 0 || !f8_type_ok(type)) return OZ2_INVALID_ARG;
     I8Args args{};
     if (oz2_status st = i8_groups(rows, groups, offsets, &args.groups)) return st;
@@ -1278,11 +1282,16 @@ oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t group
     if (rows > kF8MaxRows || i8_too_many(groups, n) || k > kI8MaxK) return OZ2_UNSUPPORTED;
     args.m = (int)rows; args.n = (int)n; args.k = (int)k;
     args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
-    return i8_launch(I8Mode::kRows, args, i8_grouped_form(I8Mode::kRows, args), stream);
+    return i8_run(resolve(ctx), I8Mode::kRows, args, stream);
 }
 
-oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+oz2_status oz2_i8_grouped_gemm(int64_t rows, int64_t n, int64_t k, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
                                const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
+    return oz2_ctx_i8_grouped_gemm(nullptr, rows, n, k, groups, offsets, alpha, A, B, beta, C, ldc, type, stream);
+}
+
+oz2_status oz2_ctx_i8_grouped_grad(oz2_context *ctx, int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+                                   const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
     if (m < 0 || n < 0 || rows < 0 || !f8_type_ok(type)) return OZ2_INVALID_ARG;
     I8Args args{};
     if (oz2_status st = i8_groups(rows, groups, offsets, &args.groups)) return st;
@@ -1296,12 +1305,26 @@ oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t group
     }
     args.m = (int)m; args.n = (int)n; args.k = (int)rows;
     args.out.C = C; args.out.ldc = ldc; args.out.type = type; args.out.alpha = alpha; args.out.beta = beta;
-    return i8_launch(I8Mode::kSums, args, i8_grouped_form(I8Mode::kSums, args), stream);
+    return i8_run(resolve(ctx), I8Mode::kSums, args, stream);
+}
+
+oz2_status oz2_i8_grouped_grad(int64_t m, int64_t n, int64_t rows, int64_t groups, const int32_t *offsets, float alpha, const oz2_i8 *A,
+                               const oz2_i8 *B, float beta, void *C, int64_t ldc, oz2_type type, hipStream_t stream) {
+    return oz2_ctx_i8_grouped_grad(nullptr, m, n, rows, groups, offsets, alpha, A, B, beta, C, ldc, type, stream);
 }
 
 size_t oz2_i8_workspace_bytes(int64_t m, int64_t n, int64_t k) {
     if (m <= 0 || n <= 0 || k <= 0 || m > kF8MaxRows || n > kF8MaxRows || k > kI8MaxK) return 0;
     return i8_plan(m, n, k).plane_bytes;
+}
+
+size_t oz2_i8_grouped_workspace_bytes(int64_t rows, int64_t n, int64_t k, int64_t groups, int grad) {
+    if (rows <= 0 || n <= 0 || k <= 0 || groups < 1 || rows > kF8MaxRows || groups > kI8MaxGroups || i8_too_many(groups, n) || i8_too_many(groups, k)) return 0;
+    if (!grad && k > kI8MaxK) return 0;
+    I8Args args{};
+    args.groups = I8Groups{nullptr, (int)groups, (int)rows, 0};
+    args.m = grad ? (int)k : (int)rows; args.n = (int)n; args.k = grad ? (int)rows : (int)k;
+    return i8_grouped_plan(grad ? I8Mode::kSums : I8Mode::kRows, args).plane_bytes;
 }
 
 }  // extern "C"

@@ -35,7 +35,7 @@ struct I8Args {
     I8Matrix A, B;
     int m, n, k;                           // kRows: m = rows of A at most; kSums: k = the most that a group may have
     I8Groups groups;
-    int ranges, kb_each;                   // kDense: K ranges and their length in blocks
+    int ranges, kb_each;                   // K ranges and their length in blocks (kSums: each group's own)
     int only_short;                        // kSums: groups that large tiles take have been served
     int turn;                              // large tiles of a round (one to a compute unit); kDense, kRows: if a last round is short, tiles of kMiddle take its place
     F8Out out;                             // (planes hold int32 sums)
@@ -84,7 +84,7 @@ inline bool i8_large_possible(I8Mode mode, const I8Args &a) {
 
 struct I8Plan {
     I8Form form;
-    int ranges, kb_each;                   // K ranges, and blocks of each
+    int ranges, kb_each;                   // K ranges, and blocks of each (kSums: 0)
     size_t plane_bytes;                    // workspace for the planes of the ranges (0: none needed)
     double us;                             // what it is expected to take
 };
@@ -144,33 +144,52 @@ inline I8Plan i8_plan_one_range(int64_t m, int64_t n, int64_t k) {
 // Products by group, from the mean of their rows, by the costs of single ones (us; small | middle | large): kRows, 64 groups, 2048 x 2048, mean 24 51 | 44 | 67, 64 68 | 56 | 69, 256 160 | 132 | 102;
 // 8 groups, 2048 x 1024, mean 100 6.8 | 7.2 | 17, 800 30 | 30 | 23; 8 groups, 8192 x 4096, mean 256 147 | 122 | 100.  kSums, 8 groups, 4096 x 2048, mean 400 74 | 72 | 82, 800
 // 112 | 102 | 95, 2000 214 | 190 | 142; 16 groups, 256 x 512, mean 800 9.2 | 11.3 | 32.
-inline I8Form i8_grouped_form(I8Mode mode, const I8Args &a) {
+// Few tiles and a long contraction go by ranges of k, too (kSums: as many for every group, of its own blocks), us without | with: kSums, 2 groups of 32768 rows, 100 x 100 68 | 12;
+// one of 16384, 1000 x 1000 53 | 36; kRows, 3 groups of 40, 64 x 8192 18.9 | 8.5.  Near the border they lose a little (8 groups of 64, 512 x 4096 11.2 | 13.2), hence 1.2.
+inline I8Plan i8_grouped_plan(I8Mode mode, const I8Args &a) {
     const int64_t rows = a.groups.rows, groups = a.groups.groups, mean = rows / groups, sought = std::min(groups, rows);
-    // Thin | small: 64 groups, 4096 x 2048, 1 row 3.9 | 7.0, 32 rows 29 | 29, 256 rows 102 | 88; 4 groups, 512 x 512, 32 rows 3.1 | 4.1; 8 groups, 8192 x 4096, 8 rows 33 | 25.
-    if (mode == I8Mode::kRows && a.k > 0 && (mean < 2 || (mean <= 8 && groups * a.n * (int64_t)a.k <= 1 << 21))) return I8Form::kThin;
     const int64_t blocks = mode == I8Mode::kRows ? i8_blocks(a.k) : i8_blocks(mean);
-    I8Form best = I8Form::kSmall;
-    double least = 1e30;
+    I8Plan best{I8Form::kThin, 1, (int)std::max<int64_t>(i8_blocks(a.k), 1), 0, 1e30};
+    // Thin | small: 64 groups, 4096 x 2048, 1 row 3.9 | 7.0, 32 rows 29 | 29, 256 rows 102 | 88; 4 groups, 512 x 512, 32 rows 3.1 | 4.1; 8 groups, 8192 x 4096, 8 rows 33 | 25.
+    if (mode == I8Mode::kRows && a.k > 0 && (mean < 2 || (mean <= 8 && groups * a.n * (int64_t)a.k <= 1 << 21))) return best;
     for (const I8Cost &c : kI8Costs) {
         if (c.form == I8Form::kLarge && (!i8_large_possible(mode, a) || mean < (mode == I8Mode::kRows ? 64 : 768))) continue;
         const int high = i8_tile_rows(c.form);
         const int64_t units = mode == I8Mode::kRows ? std::max(f8_ceil(2 * rows + sought * high, 2 * high), sought) : f8_ceil(a.m, high) * groups;
-        const int64_t tiles = units * f8_ceil(a.n, i8_tile_cols(c.form)), round = 256 * c.share, rounds = tiles / round, rest = f8_ceil(tiles - rounds * round, 256);
-        const double whole = c.per_tile + blocks * (c.first_block + (c.share - 1) * c.further_block);
-        double us = c.once + rounds * whole;
-        if (rest) us += c.per_tile + blocks * (c.first_block + (rest - 1) * c.further_block);
-        // (by rows the number of tiles is an estimate, and what units share of a weight is read more often)
-        if (mode == I8Mode::kRows && rounds == 0 && c.form == I8Form::kMiddle) us *= 1.12;
-        if (mode == I8Mode::kRows && rounds > 0) us = c.once + (c.form == I8Form::kSmall ? 1.35 : c.form == I8Form::kMiddle ? 1.2 : 1.08) * ((double)tiles / round + 0.3) * whole;
-        if (us < least) { least = us; best = c.form; }
+        const int64_t tiles = units * f8_ceil(a.n, i8_tile_cols(c.form)), round = 256 * c.share;
+        const int64_t most = c.form == I8Form::kLarge || tiles > 256 ? 1 : std::min<int64_t>(std::max<int64_t>(blocks / 2, 1), kI8MaxRanges);
+        int64_t last = 0;
+        for (int64_t asked = 1; asked <= most; ++asked) {
+            const int64_t each = std::max<int64_t>(f8_ceil(blocks, asked), 1), ranges = std::max<int64_t>(f8_ceil(blocks, each), 1);
+            if (ranges == last) continue;
+            last = ranges;
+            const int64_t items = tiles * ranges, rounds = items / round, rest = f8_ceil(items - rounds * round, 256);
+            const size_t planes = ranges == 1 ? 0 : (size_t)ranges * (size_t)(mode == I8Mode::kRows ? rows : groups * a.m) * (size_t)i8_plane_ld(a.n) * 4;
+            const double whole = c.per_tile + each * (c.first_block + (c.share - 1) * c.further_block);
+            double us = c.once + rounds * whole;
+            if (rest) us += c.per_tile + each * (c.first_block + (rest - 1) * c.further_block);
+            // (by rows the number of tiles is an estimate, and what units share of a weight is read more often)
+            if (mode == I8Mode::kRows && rounds == 0 && c.form == I8Form::kMiddle) us *= 1.12;
+            if (mode == I8Mode::kRows && rounds > 0) us = c.once + (c.form == I8Form::kSmall ? 1.35 : c.form == I8Form::kMiddle ? 1.2 : 1.08) * ((double)items / round + 0.3) * whole;
+            if (planes) us = 1.2 * (us + kI8RangesOnce + planes / kI8PlaneBytesPerUs);
+            if (us < best.us) best = I8Plan{c.form, (int)ranges, mode == I8Mode::kRows ? (int)each : 0, planes, us};
+        }
     }
     return best;
 }
+// The same without planes.
+inline I8Plan i8_grouped_plan_one_range(I8Mode mode, const I8Args &a) {
+    I8Plan p = i8_grouped_plan(mode, a);
+    p.ranges = 1;
+    p.kb_each = (int)std::max<int64_t>(i8_blocks(a.k), 1);
+    p.plane_bytes = 0;
+    return p;
+}
 // Workgroups of a launch.
 inline int64_t i8_tiles(I8Mode mode, I8Form form, const I8Args &a) {
-    const int64_t tiles_n = f8_ceil(a.n, i8_tile_cols(form));
-    if (mode == I8Mode::kRows) return f8_ceil(i8_most_units(a.groups.rows, a.groups.groups, i8_tile_rows(form)) * tiles_n, 8) * 8;
-    return f8_ceil(a.m, i8_tile_rows(form)) * tiles_n * (mode == I8Mode::kSums ? a.groups.groups : a.ranges);
+    const int64_t tiles_n = f8_ceil(a.n, i8_tile_cols(form)), ranges = std::max(a.ranges, 1);
+    if (mode == I8Mode::kRows) return f8_ceil(i8_most_units(a.groups.rows, a.groups.groups, i8_tile_rows(form)) * tiles_n, 8) * 8 * ranges;
+    return f8_ceil(a.m, i8_tile_rows(form)) * tiles_n * (mode == I8Mode::kSums ? a.groups.groups : 1) * ranges;
 }
 
 // Conversions: numbers of a row that 256 threads hold, 8 each and 1, 2, 4 or 8 times.
@@ -236,7 +255,7 @@ inline int64_t i8_quantize_threads(const I8Quantize &p) {
 hipError_t launch_i8_thin(I8Mode mode, const I8Args &args, hipStream_t stream);
 hipError_t launch_i8_wide(I8Mode mode, const I8Args &args, hipStream_t stream);
 hipError_t i8_units(int *units);              // compute units of the current device, in whole rounds of the XCDs
-hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream);
+hipError_t launch_i8_product(I8Mode mode, I8Args args, I8Form form, hipStream_t stream);   // args.ranges, kb_each and out.planes as planned
 hipError_t launch_i8_quantize(const I8Quantize &args, int type, hipStream_t stream);
 #endif
 

@@ -65,6 +65,11 @@ __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, i
     if constexpr (MODE == I8Mode::kRows) {
         const uint32_t tiles_n = (uint32_t)(p.n + BROAD - 1) / BROAD;
         I8Place at;
+        if (!LAST && p.ranges > 1) {                                       // (the grid has a part of its own for each, of whole eights)
+            const int part = (int)gridDim.x / p.ranges;
+            t.range = id / part;
+            id -= t.range * part;
+        }
         if constexpr (LAST) {
             const bool found = i8_find_place(p.groups, HIGH, tiles_n, [&](uint32_t total) {
                 const uint32_t share = (total + 7) / 8, left = i8_left_over(share, (uint32_t)p.turn / 8), local = (uint32_t)(id >> 3) / PARTS;
@@ -84,8 +89,8 @@ __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, i
         t.scale_a = p.A.scale + row0;
         t.scale_b = p.B.scale + b_row;
         t.k = p.k;
-        t.kb0 = 0;
-        t.kb1 = (p.k + kI8Block - 1) / kI8Block;
+        t.kb0 = t.range * p.kb_each;
+        t.kb1 = min(t.kb0 + p.kb_each, (p.k + kI8Block - 1) / kI8Block);
         t.c_row = row0;
         t.c_col = col0;
     } else {
@@ -106,15 +111,20 @@ __device__ __forceinline__ bool find_tile(const I8Args &p, const TileMap &map, i
             t.range = s;
             t.c_row = row0;
         } else {
+            if (p.ranges > 1) {
+                t.range = s / p.groups.groups;
+                s -= t.range * p.groups.groups;
+            }
             const I8Span span = i8_span(p.groups, s);
             if (p.only_short && i8_by_large_tiles(span.hi - span.lo)) return false;
             first = i8_first_col(span);
             scales_a = s * p.A.ld_scale;
             scales_b = s * p.B.ld_scale;
             t.lost = span.hi - span.lo > kI8MaxK;
-            t.kb0 = 0;
-            t.kb1 = t.lost ? 0 : (span.hi - span.lo + kI8Block - 1) / kI8Block;
-            t.k = t.kb1 * kI8Block;                                        // (zeros follow up to there)
+            const int KB = t.lost ? 0 : (span.hi - span.lo + kI8Block - 1) / kI8Block, each = p.ranges > 1 ? (KB + p.ranges - 1) / p.ranges : KB;
+            t.kb0 = min(t.range * each, KB);
+            t.kb1 = min(t.kb0 + each, KB);
+            t.k = KB * kI8Block;                                           // (zeros follow up to there)
             t.c_row = (int64_t)s * p.m + row0;
         }
         t.a = p.A.q + row0 * p.A.ld + first;
@@ -245,7 +255,7 @@ __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, Ti
         constexpr int N = sizeof(sum) / sizeof(sum[0]);
         const int valid = row < t.rows ? t.cols - col : 0;
         if (valid <= 0) return;
-        if (MODE == I8Mode::kDense && o.planes) {                          // (a plane's rows are stored to a multiple of 16)
+        if (o.planes) {                                                    // (a plane's rows are stored to a multiple of 16)
             int32_t *const to = reinterpret_cast<int32_t *>(o.planes) + t.range * o.plane + (t.c_row + row) * o.ldp + t.c_col + col;
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
@@ -315,12 +325,31 @@ hipError_t launch_tiles(const I8Args &args, I8Form form, hipStream_t stream) {
 }
 
 // The sums of the K ranges, and what the tiles do with a sum.  A thread has 4 columns of a row.
+template <I8Mode MODE>
 __global__ __launch_bounds__(256) void k_i8_ranges(I8Args p) {
     const int per_row = (p.n + 3) / 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / per_row;
-    if (row >= p.m) return;
+    if (row >= (MODE == I8Mode::kSums ? (int64_t)p.m * p.groups.groups : p.m)) return;
     const int col = (int)(id - row * per_row) * 4, valid = p.n - col;
     const int32_t *const from = reinterpret_cast<const int32_t *>(p.out.planes) + row * p.out.ldp + col;
+    F8Out o = p.out;
+    const float *scale_a = p.A.scale + row, *scale_b = p.B.scale + col;
+    bool lost = false, nothing = false;
+    if constexpr (MODE == I8Mode::kRows) {                     // the last group that begins at the row or before it
+        int g = 0;
+        for (int step = 1 << 12; step; step /= 2)
+            if (g + step < p.groups.groups && i8_span(p.groups, g + step).lo <= row) g += step;
+        const I8Span span = i8_span(p.groups, g);
+        if (row < span.lo || row >= span.hi) return;
+        scale_b += (int64_t)g * p.n;
+    } else if constexpr (MODE == I8Mode::kSums) {
+        const int64_t g = row / p.m;
+        const I8Span span = i8_span(p.groups, (int)g);
+        lost = span.hi - span.lo > kI8MaxK;
+        nothing = span.hi == span.lo;
+        scale_a += g * (p.A.ld_scale - p.m);
+        scale_b += g * p.B.ld_scale;
+    }
     f8_v4i s{0, 0, 0, 0};
     for (int r0 = 0; r0 < p.ranges; r0 += 4) {                 // four loads at a time: one after the other costs a way to memory each
         f8_v4i x[4];
@@ -331,7 +360,11 @@ __global__ __launch_bounds__(256) void k_i8_ranges(I8Args p) {
             if (r0 + r < p.ranges) s += x[r];
     }
     const int sum[4] = {s[0], s[1], s[2], s[3]};
-    i8_finish_row<4>(p.out, row * p.out.ldc + col, sum, p.A.scale[row], p.B.scale + col, valid);
+    if (nothing) {                                             // no infinity or NaN from alpha or from scales
+        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        o.alpha = 0.0f;
+        f8_update_row<4>(o, row * o.ldc + col, x, valid);
+    } else i8_finish_row<4>(o, row * o.ldc + col, sum, lost ? __builtin_nanf("") : *scale_a, scale_b, valid);
 }
 
 // Tiles of 64 x 64 by four wavefronts of 32 x 32, with as many stages as leave all tiles of a call on the device at once, two at least; of 64 x 128 with three.
@@ -344,11 +377,11 @@ hipError_t launch_form(const I8Args &args, I8Form form, hipStream_t stream) {
                        : tiles <= 768            ? launch_tiles<2, 2, 2, 2, 3, 3, MODE>(args, form, stream)
                                                  : launch_tiles<2, 2, 2, 2, 2, 4, MODE>(args, form, stream)) return e;
     if constexpr (MODE != I8Mode::kSums) {
-        if (form == I8Form::kLarge && args.ranges <= 1) return launch_tiles<2, 2, 2, 4, 3, 2, MODE, true>(args, I8Form::kMiddle, stream);
+        if (form == I8Form::kLarge && args.ranges == 1) return launch_tiles<2, 2, 2, 4, 3, 2, MODE, true>(args, I8Form::kMiddle, stream);
     }
-    if (MODE != I8Mode::kDense || args.ranges <= 1) return hipSuccess;
-    const int64_t threads = (int64_t)args.m * ((args.n + 3) / 4);
-    hipLaunchKernelGGL(k_i8_ranges, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, args);
+    if (args.ranges <= 1) return hipSuccess;
+    const int64_t threads = (int64_t)args.m * (MODE == I8Mode::kSums ? args.groups.groups : 1) * ((args.n + 3) / 4);
+    hipLaunchKernelGGL(k_i8_ranges<MODE>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, args);
     return hipGetLastError();
 }
 

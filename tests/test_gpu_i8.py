@@ -355,3 +355,70 @@ def test_product_in_ranges_of_k(m, n, k, dtype):
             results.append(c.clone())
             outside_kept(c, buf, before)
         assert torch.equal(results[0], results[1]) and torch.equal(results[0], results[2])  # (integer sums are exact in any order)
+
+
+def in_contexts(call):
+    """The call in the default context, in one of its own and in one without room for planes: the same bits."""
+    own, small, room = oz.Context(), oz.Context(), torch.empty(1 << 12, dtype=torch.uint8, device="cuda")
+    oz.oz2_ctx_set_workspace(small, room)
+    got = [call(ctx) for ctx in (None, own, small)]
+    assert torch.equal(got[0].view(torch.uint8), got[1].view(torch.uint8)) and torch.equal(got[0].view(torch.uint8), got[2].view(torch.uint8))
+    return got[0]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offsets,n,k", [([3, 40, 40, 90], 64, 8192), ([0, 200, 200, 200, 201], 130, 9001), ([0, 0, 64], 33, 40000)])
+def test_grouped_in_ranges_of_k(offsets, n, k, dtype):
+    rows, groups, g = offsets[-1] + 5, len(offsets) - 1, gen(k)
+    assert oz.oz2_i8_grouped_workspace_bytes(rows, n, k, groups) > 0
+    a, b = operand(g, rows, k), operand(g, groups * n, k)
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    old = torch.randn(rows, n, device="cuda", generator=g).mul_(50).to(dtype)
+    for alpha, beta in ((2.0 ** -20, 0.0), (-2.0 ** -19, 0.75)):
+        def call(ctx):
+            c = old.clone()
+            oz.oz2_ctx_i8_grouped_gemm(ctx, rows, n, k, groups, off, alpha, a, b, beta, c, n)
+            return c
+        c = in_contexts(call)
+        for i in range(groups):
+            lo, hi = offsets[i], offsets[i + 1]
+            if lo < hi:
+                summed = R.product((a.q[lo:hi], a.scale[lo:hi]), (b.q[i * n:(i + 1) * n], b.scale[i * n:(i + 1) * n]))
+                want = alpha * summed + beta * old[lo:hi].double()
+                R.check(c[lo:hi], want, R.bound(summed, want, dtype, alpha, beta))
+        assert torch.equal(c[:offsets[0]], old[:offsets[0]]) and torch.equal(c[offsets[-1]:], old[offsets[-1]:])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offsets,m,n", [([0, 3000, 8000], 26, 139), ([5, 5, 4000, 4001, 4001, 9000], 100, 100), ([0, 30000], 64, 65), ([7, 140000, 140100], 20, 30)])
+def test_grouped_grad_in_ranges(offsets, m, n, dtype):
+    rows, groups, g = offsets[-1] + 5, len(offsets) - 1, gen(m)
+    assert oz.oz2_i8_grouped_workspace_bytes(rows, n, m, groups, True) > 0
+    wide = oz.oz2_i8_grouped_cols(rows, groups)
+    a, b = operand(g, m, wide, groups), operand(g, n, wide, groups)
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    for i in range(groups):
+        first, count = R.first_col(offsets, i), offsets[i + 1] - offsets[i]
+        for x in (a, b):
+            x.q[:, first + count:first + (count + 127) // 128 * 128] = 0
+            if count == 0:
+                x.scale[i] = float("nan")                     # (the scales of nothing are not read)
+    old = torch.randn(groups * m, n, device="cuda", generator=g).mul_(50).to(dtype)
+    for alpha, beta in ((2.0 ** -20, 0.0), (-2.0 ** -19, 0.75)):
+        def call(ctx):
+            c = old.clone()
+            oz.oz2_ctx_i8_grouped_grad(ctx, m, n, rows, groups, off, alpha, a, b, beta, c, n)
+            return c
+        c = in_contexts(call)
+        for i in range(groups):
+            part = slice(R.first_col(offsets, i), R.first_col(offsets, i) + offsets[i + 1] - offsets[i])
+            own, mine = c[i * m:(i + 1) * m], old[i * m:(i + 1) * m].double()
+            if offsets[i + 1] - offsets[i] > 131071:
+                assert torch.isnan(own).all()
+            elif offsets[i + 1] == offsets[i]:
+                assert torch.equal(own, (beta * mine).to(dtype))
+            else:
+                scale = (a.scale, b.scale) if groups == 1 else (a.scale[i], b.scale[i])
+                summed = R.product((a.q[:, part], scale[0]), (b.q[:, part], scale[1]))
+                want = alpha * summed + beta * mine
+                R.check(own, want, R.bound(summed, want, dtype, alpha, beta))

@@ -25,8 +25,9 @@ int main() {
             x.groups.rows = a; x.groups.groups = b;
             const I8Mode mode = what == 'r' ? I8Mode::kRows : I8Mode::kSums;
             if (what == 'r') { x.m = a; x.n = c; x.k = d; } else { x.m = c; x.n = d; x.k = a; }
-            const I8Form f = i8_grouped_form(mode, x);
-            printf("%%d %%ld\n", (int)f, (long)i8_tiles(mode, f, x));
+            const I8Plan p = i8_grouped_plan(mode, x);
+            x.ranges = p.ranges;
+            printf("%%d %%ld %%d %%ld\n", (int)p.form, (long)i8_tiles(mode, p.form, x), p.ranges, (long)p.plane_bytes);
         } else {                                               // rows cols groups, both forms (q: by group, b: a batch)
             I8Quantize q{};
             q.q = q.qt = reinterpret_cast<int8_t *>(&x);
@@ -67,9 +68,9 @@ def test_sizes_of_the_gpu_tests_take_every_form(plan):
     assert any(m % 256 and n % 256 and k % 128 for (m, n, k), p in zip(sizes, got) if p[0] == 3)
     rows = [(o[-1] + 7, len(o) - 1, n, k) for o in large.LONG for n, k in ((2048, 384), (1111, 1000), (2300, 513), (5000, 640), (7000, 400))]
     rows += [(o[-1] + 7, len(o) - 1, n, k) for o in GROUPS for n, k in ((1, 1), (70, 130), (300, 257), (129, 1000))]
-    assert {f for f, _ in plan("r", rows)} == {0, 1, 2, 3}
+    assert {f for f, *_ in plan("r", rows)} == {0, 1, 2, 3}
     sums = [(o[-1] + 7, len(o) - 1, m, n) for o, m, n in large.SUMS + [(o, 70, 130) for o in GROUPS]]
-    assert {f for f, _ in plan("s", sums)} == {1, 2, 3}
+    assert {f for f, *_ in plan("s", sums)} == {1, 2, 3}
 
 
 def test_ranges_cover_k_and_planes_hold_them(plan):
@@ -96,3 +97,13 @@ def test_conversions_take_every_way(plan):
     assert by_batch[-2][1] > 0 and by_batch[-2][2] == 0 and by_batch[4][1] == 0 and by_batch[4][2] > 0     # maxima of columns with the rows, or apart
     assert all(p[4] < 1 << 32 for p in by_batch)
     assert [p[3] for p in plan("q", [(384 * 5, 100, 5), (384 * 5 + 1, 100, 5), (100, 100, 4096)])] == [1, 0, 1]
+
+
+def test_planes_of_grouped_products(plan):
+    sizes = [(rows, groups, n, k) for rows in (1, 100, 5000, 65536) for groups in (1, 2, 9, 500) for n in (1, 100, 1000) for k in (64, 9000)]
+    for what, grad in (("r", False), ("s", True)):
+        got = plan(what, [(r, g, n, k) if not grad else (r, g, k, n) for r, g, n, k in sizes])
+        assert any(ranges > 1 for _, _, ranges, _ in got)
+        for (rows, groups, n, k), (form, _, ranges, planes) in zip(sizes, got):
+            assert planes == (0 if ranges == 1 else ranges * (groups * k if grad else rows) * ((n + 15) // 16 * 16) * 4)
+            assert planes == oz.oz2_i8_grouped_workspace_bytes(rows, n, k, groups, grad) and (ranges == 1 or form in (1, 2))

@@ -30,9 +30,9 @@ template <int N, typename F>
 __device__ __forceinline__ void static_for(F &&f) { static_for_(f, std::make_integer_sequence<int, N>{}); }
 
 extern __shared__ f8_v4i i8_wide_lds[];                       // 2 stages of [256 rows of A | 256 rows of B][128], 1 KiB per wavefront for loads that
-                                                              // are not wanted, then the groups: kI8WideGroups + 1 first rows, as many numbers of units
+                                                              // are not wanted, the scales of the 512 rows, then the groups: kI8WideGroups + 1 first rows, as many numbers of units
 
-constexpr int kStageBytes = 512 * 128, kNowhereAt = 2 * kStageBytes, kGroupsAt = kNowhereAt + 4 * 1024;
+constexpr int kStageBytes = 512 * 128, kNowhereAt = 2 * kStageBytes, kScalesAt = kNowhereAt + 4 * 1024, kGroupsAt = kScalesAt + 512 * 4;
 constexpr size_t kWideLdsBytes = kGroupsAt + 2 * (kI8WideGroups + 1) * 4;
 
 #define OZ2_TEN(n) "a" #n "0", "a" #n "1", "a" #n "2", "a" #n "3", "a" #n "4", "a" #n "5", "a" #n "6", "a" #n "7", "a" #n "8", "a" #n "9"
@@ -286,6 +286,18 @@ struct Wide {
         static_for<8>([&](auto h) { load<8 + decltype(h)::value>(at, to, 4096); });
     }
 
+    // The scales of the tile's rows of A and B, a word for each in LDS, where they are when its second block is.  This wavefront's are 128 of either.
+    __device__ __forceinline__ void request_scales(const Item &it) const {
+        const Place p = place_of(it);
+        const float *const from = (wave < 2 ? p.scale_a : p.scale_b) + (wave & 1) * 128 + lane;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const uint32_t to = lds0 - wave * 1024 + kScalesAt + wave * 512 + half * 256;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from + half * 64) : "memory");
+        }
+    }
+    static __device__ __forceinline__ const float *scales() { return reinterpret_cast<const float *>(i8_wide_lds) + kScalesAt / 4; }
+
     struct Registers {
         f8_v4i a[2][8][2], b[8][2];
     };
@@ -422,12 +434,12 @@ struct Wide {
         float a[8];
         f8_v4f b[8];
     };
-    __device__ __forceinline__ void load_scales(const Place &p, Scales &s) const {
-        const float *const a = p.scale_a + (wave >> 1) * 128 + lrow, *const b = p.scale_b + (wave & 1) * 128 + quarter * 4;
+    __device__ __forceinline__ void read_scales(Scales &s) const {
+        const float *const a = scales() + (wave >> 1) * 128 + lrow, *const b = scales() + 256 + (wave & 1) * 128 + quarter * 4;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s.a[i] = a[i * 16];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) __builtin_memcpy(&s.b[j], b + j * 16, 16);
+        for (int j = 0; j < 8; ++j) s.b[j] = *reinterpret_cast<const f8_v4f *>(b + j * 16);
     }
     template <int I, int J>
     static __device__ __forceinline__ void take_scaled(const Scales &s, float alpha, float (&x)[16]) {
@@ -444,7 +456,7 @@ struct Wide {
     template <int TYPE>
     __device__ __forceinline__ void store_16_bits(const F8Out &o, const Place &p) const {
         Scales s;
-        load_scales(p, s);
+        read_scales(s);
         const int row = (wave >> 1) * 128 + lrow;
         uint16_t *const c = static_cast<uint16_t *>(o.C) + (p.c_row + row) * o.ldc + p.col0 + (wave & 1) * 128 + quarter * 16;
         static_for<8>([&](auto number) {
@@ -462,7 +474,7 @@ struct Wide {
     template <bool SCALED>
     __device__ __forceinline__ void store_32_bits(float *to, int64_t ld, const Place &p, float alpha) const {
         Scales s;
-        if constexpr (SCALED) load_scales(p, s);
+        if constexpr (SCALED) read_scales(s);
         const int row = (wave >> 1) * 128 + lrow;
         float *const first = to + (p.c_row + row) * ld + p.col0 + (wave & 1) * 128 + quarter * 4;
         static_for<16>([&](auto number) {
@@ -505,13 +517,13 @@ struct Wide {
         for (int unit = 0; unit < 16; ++unit) {
             float x[16];
             const int row = own_row + unit / 2 * 16;
-            const float *const scale = p.scale_b + (wave & 1) * 128 + unit % 2 * 64 + quarter * 4;
+            const float *const scale = scales() + 256 + (wave & 1) * 128 + unit % 2 * 64 + quarter * 4;
             int n[16];
             static_for<16>([&](auto number) {
                 constexpr int N = decltype(number)::value;
                 if (unit == N) take<N / 2, N % 2 * 4>(n);
             });
-            const float by = p.scale_a[row];
+            const float by = scales()[row];
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] = (float)n[e] * by * scale[e / 4 * 16 + e % 4] * alpha;
             exchange(x);
@@ -560,6 +572,7 @@ __global__ __launch_bounds__(256, 1) void k_i8_wide(WideArgs args) {
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");    // A's part is free for the third block
         w.advance_a(false);
         w.request_a();
+        w.request_scales(it);
         int kb = kb0;
         w.template block<true, 0>(f, kb, kb1, stage);
         stage ^= 1;

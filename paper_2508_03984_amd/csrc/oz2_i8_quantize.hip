@@ -4,6 +4,10 @@
 // q without a division: t = x r with r = 1 / s from the hardware, within a unit of the last place, is within 2^-22 of the quotient (relative), so n = rint(t) is q unless the quotient lies that near to the
 // middle of two integers.  e = x - n s, one fused operation, is exact there (a multiple of ulp(s) / 2 below s), so 2 |e| > s says that n is one too far from x, and
 // 2 |e| = s that x lies in the middle and the even neighbour is asked for (s / 2 may be subnormal and not exact).  rint is the addition of 1.5 2^23, which leaves q's byte at the end of the word.
+//
+// Rows are held in registers, so that they are read once; columns need a maximum over all rows before the first byte, so X is read twice where the transpose is wanted.  16384 x 4096 bf16 as it is
+// 34 us (5.9 TB/s, X partly from the last-level cache), transposed 66, both 95; 8 of 4096 x 2048 f32 both 123 to 138 us; 100 x 100 both 4.5; 64 x 8192 as it is 3.1 us.  Bound: HBM and, transposed, the conversion's own
+// instructions (about 10 a number); the smallest by launch and latency.
 #include "oz2_i8_device.hpp"
 
 namespace oz2 {

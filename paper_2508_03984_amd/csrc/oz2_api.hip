@@ -17,7 +17,7 @@
 #include "oz2_kernels.hpp"
 #include "oz2_plan.hpp"
 
-// Memory for the planes of K ranges of 8-bit floating-point products (f8_planes).
+// Memory for the planes of K ranges of products in 8 bits (f8_planes).
 struct F8Planes {
     char *ptr;
     size_t bytes;

@@ -62,7 +62,7 @@ inline int64_t i8_grouped_cols(int64_t rows, int64_t groups) { return rows / kI8
 inline int64_t i8_most_units(int64_t rows, int64_t groups, int64_t each) { return rows / each + std::min(groups, rows); }
 
 // kThin: few rows (of a group), B read once into registers, 16 columns of C (of a group) to a workgroup (oz2_i8_thin.hip).  The others tiles of C
-// of 64 x 64, 64 x 128 (oz2_i8_gemm.hip) or 256 x 256 (oz2_i8_wide.hip); kDense may cut k into ranges whose sums are added by a second kernel.
+// of 64 x 64, 64 x 128 (oz2_i8_gemm.hip) or 256 x 256 (oz2_i8_wide.hip), the smaller two, and all of kDense, over ranges of k if there are few, whose sums a second kernel adds.
 enum class I8Form { kThin, kSmall, kMiddle, kLarge };
 inline int i8_tile_rows(I8Form form) { return form == I8Form::kThin ? 1 << 30 : form == I8Form::kLarge ? 256 : 64; }
 inline int i8_tile_cols(I8Form form) { return form == I8Form::kThin ? 16 : form == I8Form::kLarge ? 256 : form == I8Form::kMiddle ? 128 : 64; }
@@ -90,6 +90,10 @@ struct I8Plan {
 };
 inline int64_t i8_plane_ld(int64_t n) { return f8_ceil(n, 16) * 16; }
 
+// What a call takes with tiles of one form, in us: something once, and for each round of the device a time per tile and per block of k; a round is `share` tiles on each of
+// 256 units, in the last one units with fewer tiles are faster per block.  Measured, 64 x 64 | 64 x 128 | 256 x 256: 500 x 300 x 777 5.7 | 8.3 | 16; 1024 x 4096 x 4096 27.7 | 23.4 | 44; 2048^3
+// 15.6 | 13.2 | 26; 3000^3 51 | 46 | 38; 4096 x 4096 x 512 20.4 | 21.5 | 19.2; 8192 x 1024 x 256 9.4 | 10.1 | -.  With ranges: 100 x 100 x 20000 42 -> 9.3 (16), 512 x 512 x 4096 11.0 -> 10.1 (3), 1536 x 1000 x 40000
+// 342 -> 69 (10, of large tiles).  Of 36 shapes the choice is within 3 % of the best of all forms and ranges, 8 % at worst (65 x 8192 x 8192 22.1 | 20.5).
 struct I8Cost {
     I8Form form;
     int share;
@@ -100,6 +104,8 @@ constexpr double kI8RangesOnce = 3.0, kI8PlaneBytesPerUs = 4.0e6;   // the secon
 constexpr double kI8BytesPerUs = 5.2e6;                        // from HBM
 constexpr int kI8MaxRanges = 16;
 
+// The form for few rows: B from HBM, or what a unit's workgroups load through its caches.  This form | the best of the others: 1 x 8192 x 8192 13.9 | 16; 33 x 2048 x 2048 5.9 | 6.8; 17 x 8192 x 8192 19.5 | 15.0;
+// 64 x 8192 x 8192 41 | 17.4; 16 x 128 x 16384 16.3 | 8.3; 8 x 300 x 700 3.1 | 5.2.
 inline double i8_thin_us(int64_t m, int64_t n, int64_t k) {
     const int64_t rounds = f8_ceil(f8_ceil(n, 16), 256), computed = m <= 16 ? 16 : m <= 32 ? 32 : 64;
     return std::max(3.0 + rounds * k * ((m + computed) / 2.0 + 8) / 2.8e4, 1.0 + (double)n * k / kI8BytesPerUs);
@@ -212,7 +218,7 @@ constexpr int kI8StripCols = 2048;
 inline I8ConvertPlan i8_convert_plan(const I8Quantize &p) {
     const int64_t rows = p.groups.rows, groups = p.groups.groups;
     I8ConvertPlan plan{p.cols <= 32 ? 4 : p.cols <= 128 ? 16 : p.cols <= 512 ? 64 : p.cols <= kI8MostHeld ? 256 : 0, 0, 0, false};
-    if (p.cols > 2048 && plan.lanes && rows <= 512) plan.lanes = 1024;
+    if (p.cols > 2048 && plan.lanes && rows <= 512) plan.lanes = 1024;    // (a row's numbers spread wider: 64 x 8192 bf16 4.5 -> 3.1 us)
     if (!p.qt) return plan;
     // Few rows to a group (by group the mean says less): one launch.  Three or four | one, us, both forms: 100 x 100 bf16 10.5 | 4.5, 512 x 4096 15.7 | 13.3, 64 of 128 x 512
     // 15.5 | 9.4, 1000 x 1000 15.1 | 16.9, 4000 x 64 12.2 | 37.7.

@@ -371,7 +371,8 @@ __global__ __launch_bounds__(256) void k_i8_ranges(I8Args p) {
     } else i8_finish_row<4>(o, row * o.ldc + col, sum, lost ? __builtin_nanf("") : *scale_a, scale_b, valid);
 }
 
-// Tiles of 64 x 64 by four wavefronts of 32 x 32, with as many stages as leave all tiles of a call on the device at once, two at least; of 64 x 128 with three.
+// Tiles of 64 x 64 by four wavefronts of 32 x 32, with as many stages as leave all tiles of a call on the device at once, two at least (two | four stages, us: 500 x 300 x 777 7.6 | 6.1; two | three, 640 tiles of
+// a gradient with 3 to 6 blocks 17.5 | 11.7); of 64 x 128 with three.  Two teams of wavefronts for alternate blocks of a tile were no faster (500 x 300 x 777 5.5 -> 5.7).
 template <I8Mode MODE>
 hipError_t launch_form(const I8Args &args, I8Form form, hipStream_t stream) {
     const int64_t tiles = i8_tiles(MODE, form, args);

@@ -254,9 +254,9 @@ __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, Ti
     __syncthreads();
     F8Out o = p.out;
     if (none) o.alpha = 0.0f;                                              // no infinity or NaN from it
-    // N numbers of a row, at a column that is a multiple of N.
-    const auto emit = [&](const auto &sum, int row, int col) {
-        constexpr int N = sizeof(sum) / sizeof(sum[0]);
+    // 16 numbers of a row, at a column that is a multiple of 16.
+    const auto emit = [&](const int (&sum)[16], int row, int col) {
+        constexpr int N = 16;
         const int valid = row < t.rows ? t.cols - col : 0;
         if (valid <= 0) return;
         if (o.planes) {                                                    // (a plane's rows are stored to a multiple of 16)
@@ -278,33 +278,25 @@ __global__ __launch_bounds__(WM *WN * 64, PER_SIMD) void k_i8_tiles(I8Args p, Ti
         }
         f8_update_row<N>(o, (t.c_row + row) * o.ldc + t.c_col + col, x, valid);
     };
-    if constexpr (FN == 1) {                                               // 4 numbers of a row per lane, as they are
+    // Four blocks at a time, exchanged so that quarter q of the wavefront has 16 columns of block q's rows: blocks (i, j) to (i, j + 3),
+    // or, of two columns of blocks, (i, 0), (i, 1), (i + 1, 0), (i + 1, 1).
+    constexpr int GI = FN >= 4 ? 1 : 2, GJ = 4 / GI;
+    static_assert(FM % GI == 0 && FN % GJ == 0, "");
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int x[4] = {acc[i][0][0], acc[i][0][1], acc[i][0][2], acc[i][0][3]};
-            emit(x, (wm * FM + i) * 16 + lrow, wn * 16 + quarter * 4);
-        }
-    } else {
-        // Four blocks at a time, exchanged so that quarter q of the wavefront has 16 columns of block q's rows: blocks (i, j) to (i, j + 3),
-        // or, of two columns of blocks, (i, 0), (i, 1), (i + 1, 0), (i + 1, 1).
-        constexpr int GI = FN >= 4 ? 1 : 2, GJ = 4 / GI;
-        static_assert(FM % GI == 0 && FN % GJ == 0, "");
+    for (int i = 0; i < FM; i += GI)
 #pragma unroll
-        for (int i = 0; i < FM; i += GI)
+        for (int j = 0; j < FN; j += GJ) {
+            int x[16];
 #pragma unroll
-            for (int j = 0; j < FN; j += GJ) {
-                int x[16];
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t d[4] = {(uint32_t)acc[i][j][r], (uint32_t)acc[i][j + 1][r], (uint32_t)acc[i + (GI - 1)][GJ == 4 ? j + 2 : j][r],
+                                       (uint32_t)acc[i + (GI - 1)][GJ == 4 ? j + 3 : j + 1][r]};
+                const exchanged_t e = exchange_quarters(d);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t d[4] = {(uint32_t)acc[i][j][r], (uint32_t)acc[i][j + 1][r], (uint32_t)acc[i + (GI - 1)][GJ == 4 ? j + 2 : j][r],
-                                           (uint32_t)acc[i + (GI - 1)][GJ == 4 ? j + 3 : j + 1][r]};
-                    const exchanged_t e = exchange_quarters(d);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) x[4 * q + r] = e[q];
-                }
-                emit(x, (wm * FM + i + quarter / GJ) * 16 + lrow, (wn * FN + j + quarter % GJ) * 16);
+                for (int q = 0; q < 4; ++q) x[4 * q + r] = e[q];
             }
-    }
+            emit(x, (wm * FM + i + quarter / GJ) * 16 + lrow, (wn * FN + j + quarter % GJ) * 16);
+        }
 }
 
 template <int WM, int WN, int FM, int FN, int STAGES, int PER_SIMD, I8Mode MODE, bool LAST = false>

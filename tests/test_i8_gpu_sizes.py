@@ -33,3 +33,14 @@ def test_conversions_take_every_form(plan):  # noqa: F811
     from test_gpu_i8 import SIZES
     lanes = {(p[0], c > 8192) for p, (_, c) in zip(plan("b", [(r, c, 1) for r, c in SIZES]), SIZES) if p[3]}
     assert {(1024, False), (1024, True), (0, True)} <= lanes
+
+
+def test_many_groups_take_large_tiles(plan):  # noqa: F811
+    import test_gpu_i8_many_groups as T
+    for what, sizes in (("r", T.ROWS), ("s", T.SUMS)):
+        got = plan(what, [(T.offsets_of(g, mean)[-1] + 7, g, a, b) for g, mean, a, b in sizes])
+        assert [(form, ranges) for form, _, ranges, _ in got] == [(3, 1)] * len(sizes), got
+        for groups, mean, *_ in sizes:
+            of = T.lengths(groups, mean)
+            assert min(of) == 0 and of.count(0) < groups / 4 and (groups < 67 or of[62:67] == [0, 300, 0, 259, 1])
+            assert what == "r" or any(0 < n <= 256 for n in of)  # (which are left to smaller tiles)

@@ -44,3 +44,32 @@ def test_many_groups_take_large_tiles(plan):  # noqa: F811
             of = T.lengths(groups, mean)
             assert min(of) == 0 and of.count(0) < groups / 4 and (groups < 67 or of[62:67] == [0, 300, 0, 259, 1])
             assert what == "r" or any(0 < n <= 256 for n in of)  # (which are left to smaller tiles)
+
+
+def span(offsets, g, rows):
+    """The rows that a group is taken to have, whatever the offsets are."""
+    lo = min(max(offsets[g], 0), rows)
+    return lo, min(max(offsets[g + 1], lo), rows)
+
+
+def test_bad_offsets_meet_every_form_and_stay_inside(plan):  # noqa: F811
+    import test_gpu_i8_bad_offsets as T
+    rows = [(form, ranges > 1) for form, _, ranges, _ in plan("r", T.ROWS)]
+    assert rows == [(0, False), (1, False), (2, False), (3, False), (3, False), (1, True)], rows
+    sums = [(form, ranges > 1) for form, _, ranges, _ in plan("s", T.SUMS)]
+    assert sums == [(1, False), (2, False), (3, False), (3, False), (1, True)], sums
+    got = plan("q", [(r, c, g) for r, g, c in T.CONVERSIONS])
+    assert [(p[3], p[1] > 0, p[2] > 0) for p in got] == [(1, 0, 0), (0, 1, 0), (0, 1, 0), (0, 0, 1), (0, 0, 1)], got
+    left = []
+    for n_rows, groups, n, _ in T.ROWS[3:5]:                   # of large tiles: those that a last round leaves to smaller ones, on 256 units
+        for bad in T.bad_offsets(n_rows, groups):
+            units = sum(-(-(hi - lo) // 256) for lo, hi in (span(bad, g, n_rows) for g in range(groups)))
+            share = (units * -(-n // 256) + 7) // 8
+            left.append(share % 32 if share > 32 and share % 32 <= 12 else 0)
+    assert any(left)
+    for n_rows, groups, *_ in T.ROWS + T.SUMS + T.CONVERSIONS:
+        wide = n_rows // 128 * 128 + 128 * groups
+        for bad in T.bad_offsets(n_rows, groups):
+            for g in range(groups):
+                lo, hi = span(bad, g, n_rows)
+                assert 0 <= lo <= hi <= n_rows and (lo // 128 + g) * 128 + (hi - lo + 127) // 128 * 128 <= wide

@@ -73,3 +73,28 @@ def test_bad_offsets_meet_every_form_and_stay_inside(plan):  # noqa: F811
             for g in range(groups):
                 lo, hi = span(bad, g, n_rows)
                 assert 0 <= lo <= hi <= n_rows and (lo // 128 + g) * 128 + (hi - lo + 127) // 128 * 128 <= wide
+
+
+def test_overflows_and_far_operands_meet_every_form(plan):  # noqa: F811
+    import test_gpu_i8_far_large as F
+    import test_gpu_i8_overflow as T
+    got = plan("d", T.PRODUCTS + [(F.ROWS, F.N, F.K), (F.N, F.ROWS, F.K)])
+    assert [(p[0], p[1] > 1) for p in got] == [(0, False), (1, False), (2, False), (3, False), (1, True), (3, True), (3, False), (3, False)], got
+    got = plan("r", [(o[-1] + 2, len(o) - 1, n, k) for o, n, k in T.ROWS])
+    assert [(form, ranges > 1) for form, _, ranges, _ in got] == [(0, False), (1, False), (2, False), (1, True), (3, False)], got
+    got = plan("s", [(o[-1] + 2, len(o) - 1, m, n) for o, m, n in T.SUMS] + [(F.TOKENS, 2, F.M, F.N), (F.TOKENS, 2, F.N, F.M)])
+    assert [(form, ranges > 1) for form, _, ranges, _ in got] == [(1, False), (2, False), (1, True), (3, False), (3, False), (3, False)], got
+
+
+def test_the_check_of_overflows_passes_over_nothing():
+    import pytest
+    import torch
+    import test_gpu_i8_overflow as T
+    want = torch.tensor([[1.0, 1e6, -1e6, 65510.0]], dtype=torch.float64)
+    right = torch.tensor([[1.0, float("inf"), -float("inf"), 65504.0]], dtype=torch.float16)
+    T.check(right, want, want)
+    for i, wrong in ((1, 0.0), (1, 65504.0), (1, -float("inf")), (2, float("inf")), (3, float("inf")), (0, float("inf")), (0, 1.01), (1, float("nan"))):
+        bad = right.clone()
+        bad[0, i] = wrong
+        with pytest.raises(AssertionError):
+            T.check(bad, want, want)

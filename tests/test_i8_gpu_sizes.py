@@ -1,5 +1,4 @@
 """That the sizes of the GPU tests of 8-bit integers take the forms which those tests are for, by the plans on the CPU: another fit of the plans must not leave a form untested."""
-from test_i8_forms import plan  # noqa: F401"""That the sizes of the GPU tests of 8-bit integers take the forms which those tests are for, by the plans on the CPU: another fit of the plans must not leave a form untested."""
 from test_i8_forms import plan  # noqa: F401
 
 

@@ -391,7 +391,8 @@ size_t oz2_f8_workspace_bytes(int64_t m, int64_t n, int64_t k, int gated);
  * Products in 8-bit integers with a scale for each token and channel, alone and grouped by expert.  Conventions as above.
  *
  * oz2_i8: a rows x k matrix of integers, entry (r, h) standing for q[r * ld + h] * scale[r].  q is 16-byte aligned and ld a multiple of 16, at least
- * k and at most 2^23.  Rows are stored up to the next multiple of 16 bytes: what lies between is read and has no effect.  Where rows
+ * k and at most 2^23.  Rows are stored up to the next multiple of 16 bytes: what lies between is read and has no effect.  (So a matrix without gaps between its rows is taken only
+ * if k is a multiple of 16; others are copied to such rows once.)  Where rows
  * lie side by side by groups (oz2_i8_quantize_grouped, transposed; oz2_i8_grouped_grad) group g has scales of its own, scale[g * ld_scale + r] with
  * ld_scale >= rows; elsewhere ld_scale has no meaning.  The struct is read during the call only.
  *
@@ -410,7 +411,8 @@ typedef struct {
 /*
  * `batch` matrices of rows x cols numbers of `type`, one below the other in X (ldx >= cols), in 8-bit integers: as they are (batch * rows x cols),
  * each transposed (batch * cols x rows, one below the other), or both; the other pointer is NULL.  The scale of a row of what is written (so of
- * a column of X in the transpose) is max|x| times the binary32 number next to 1 / 127, rounded to binary32, 2^-126 at least, and q the integer next to x / scale, ties to even.  A
+ * a column of X in the transpose) is max|x| times the binary32 number next to 1 / 127, rounded to binary32, 2^-126 at least, and q the integer next to x / scale, ties to even.  (The
+ * quotient max|x| / 127 rounded once is the same or, for 4.7 % of the binary32 numbers, one unit of the last place away; 5 to 8 of 100000 integers of normal bf16 numbers then differ by one.)  A
  * row with NaN or an infinity has the scale NaN and zeros: NaN reaches the results that it belongs to.  Bytes from the end of a row to the next
  * multiple of 16 are cleared; further ones are not touched.
  */

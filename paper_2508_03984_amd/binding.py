@@ -736,7 +736,8 @@ def oz2_f8_workspace_bytes(m, n, k, gated=False) -> int:
 # ------------------------------------------------------------------ 8-bit integers
 class I8:
     """A rows x cols matrix of 8-bit integers on the device (oz2_i8): `q` (torch.int8) and `scale` (torch.float32), one for each row, or `groups` x rows for
-    the rows of groups that lie side by side.  Keep it as long as the tensors' memory: a call reads the addresses from here."""
+    the rows of groups that lie side by side.  Rows have to lie on multiples of 16 bytes (`empty` makes such memory, `of` copies other tensors to it: one without gaps whose columns are no multiple
+    of 16, say).  Keep it as long as the tensors' memory: a call reads the addresses from here."""
 
     __slots__ = ("q", "scale", "rows", "cols", "groups", "ref", "_struct")
 

@@ -150,6 +150,8 @@ inline I8Plan i8_plan_one_range(int64_t m, int64_t n, int64_t k) {
 // Products by group, from the mean of their rows, by the costs of single ones (us; small | middle | large): kRows, 64 groups, 2048 x 2048, mean 24 51 | 44 | 67, 64 68 | 56 | 69, 256 160 | 132 | 102;
 // 8 groups, 2048 x 1024, mean 100 6.8 | 7.2 | 17, 800 30 | 30 | 23; 8 groups, 8192 x 4096, mean 256 147 | 122 | 100.  kSums, 8 groups, 4096 x 2048, mean 400 74 | 72 | 82, 800
 // 112 | 102 | 95, 2000 214 | 190 | 142; 16 groups, 256 x 512, mean 800 9.2 | 11.3 | 32.
+// The host does not know who has how many rows, so one long group among short ones goes by the form of the mean: 64 groups, 4096 x 2048, 127 rows (the form for few rows, which reads a group's weight again for every
+// 16 rows), 2 each 111 us, one of 64 and 63 of 1 154.
 // Few tiles and a long contraction go by ranges of k, too (kSums: as many for every group, of its own blocks), us without | with: kSums, 2 groups of 32768 rows, 100 x 100 68 | 12;
 // one of 16384, 1000 x 1000 53 | 36; kRows, 3 groups of 40, 64 x 8192 18.9 | 8.5.  Near the border they lose a little (8 groups of 64, 512 x 4096 11.2 | 13.2), hence 1.2.
 inline I8Plan i8_grouped_plan(I8Mode mode, const I8Args &a) {
@@ -221,7 +223,8 @@ inline I8ConvertPlan i8_convert_plan(const I8Quantize &p) {
     if (p.cols > 2048 && plan.lanes && rows <= 512) plan.lanes = 1024;    // (a row's numbers spread wider: 64 x 8192 bf16 4.5 -> 3.1 us)
     if (!p.qt) return plan;
     // Few rows to a group (by group the mean says less): one launch.  Three or four | one, us, both forms: 100 x 100 bf16 10.5 | 4.5, 512 x 4096 15.7 | 13.3, 64 of 128 x 512
-    // 15.5 | 9.4, 1000 x 1000 15.1 | 16.9, 4000 x 64 12.2 | 37.7.
+    // 15.5 | 9.4, 1000 x 1000 15.1 | 16.9, 4000 x 64 12.2 | 37.7.  A long group among short ones is read by a workgroup for every 32 columns all the same: 64 groups, 800 columns, 4630 rows, about 72 each 13.4, one
+    // of 4000 and 63 of 10 63.
     if (rows <= (p.groups.offsets ? 384 : 512) * groups && rows * p.cols <= 1 << 22) {
         plan.strips = true;
         return plan;
